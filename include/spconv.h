@@ -324,6 +324,77 @@ SPCONV_API int spconv_dgrad(const void* dout, const void* weights, spconv_kmap* 
 SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km, int C_in, int C_out,
                  spconv_dtype dtype, const spconv_config* cfg_or_null, float* dweights, void* stream);
 
+/* ---- 8-bit checkpoints of activations (not part of the paper's method: they halve what a training step keeps of 16-bit
+ * activations for its backward pass).  A checkpoint of a tensor [rows][C] is
+ *   data  device int8  [rows][C]
+ *   exps  device uint8 [rows][ceil(C / 32)]
+ * Each row is cut into blocks of 32 channels (the last one shorter).  A block's b in exps is the biased fp32 exponent of its
+ * largest magnitude, at least 1; a channel's q in data, -127..127, stands for q * 2^(b - 133), exactly, in every dtype.  q is the
+ * value over the step 2^(b - 133), rounded to nearest even, at most 127 in magnitude, and +-1 where a value other than 0 would round
+ * to 0.  So a value is off by at most half a step - one step where it is kept from rounding to 128 or to 0 - which is
+ * 2^-7 (2^-6) of the block's largest magnitude; its sign is always right.  A block with an infinity or a NaN has b = 255 and
+ * q = 0, and stands for NaN throughout.
+ * C is 1 to 4096, rows * C at most 2^40.  Both pointers belong to the caller; no alignment is needed (16-byte aligned rows of
+ * tensors and 8-byte aligned rows of data are the fast case). */
+typedef struct spconv_q8 {
+  int8_t* data;
+  uint8_t* exps;
+} spconv_q8;
+
+/* out = the checkpoint of x [rows][C].  EINVAL: null pointers, sizes, dtype. */
+SPCONV_API int spconv_q8_pack(const void* x, int64_t rows, int C, spconv_dtype dtype, const spconv_q8* out, void* stream);
+
+/* out [rows][C] = the values that kept stands for.  EINVAL as above. */
+SPCONV_API int spconv_q8_unpack(const spconv_q8* kept, int64_t rows, int C, spconv_dtype dtype, void* out, void* stream);
+
+/* out[i] = q > 0 ? dout[i] : 0 for n elements: the gradient dout through a ReLU whose output was kept (spconv_ew, op 3, on the
+ * values; exactly so on the output itself, except that a block with an infinity or a NaN lets nothing through).  Reads kept->data only.
+ * out may be dout. */
+SPCONV_API int spconv_relu_bwd_q8(const void* dout, const spconv_q8* kept, void* out, int64_t n, spconv_dtype dtype, void* stream);
+
+/* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout.  The values are exact in dtype: the result is
+ * that of spconv_wgrad on the unpacked tensor. */
+SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
+                               const spconv_config* cfg_or_null, float* dweights, void* stream);
+
+/* ---- layer norm over the channels of each row (not part of the paper's method: glue between layers, like spconv_ew), with the
+ * residual add and the ReLU that stand behind it in a network:
+ *   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = act((x - m) * r * weight + bias + residual)
+ *   x, residual, y   device [rows][C] of dtype; residual may be NULL; y may be x or residual
+ *   weight, bias     device fp32 [C], each may be NULL (ones, zeros)
+ *   relu             0 or 1: act(v) = v < 0 ? 0 : v (a NaN stays a NaN)
+ *   stats            device fp32 [rows][2] receives (m, r) of each row for the backward pass; may be NULL
+ *   keep_x, keep_y   receive checkpoints of x and of y (as written) in the same pass: what spconv_q8_pack makes of them;
+ *                    each may be NULL
+ * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
+ * `stream` and allocates nothing.  EINVAL: null pointers, sizes, dtype, relu, eps negative or NaN. */
+SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual_or_null, const float* weight_or_null,
+                                     const float* bias_or_null, float eps, int relu, int64_t rows, int C, spconv_dtype dtype,
+                                     void* y, float* stats_or_null, const spconv_q8* keep_x_or_null,
+                                     const spconv_q8* keep_y_or_null, void* stream);
+
+/* Bytes of the workspace that spconv_layer_norm_bwd needs for dweight and dbias (SPCONV_EINVAL for sizes it refuses). */
+SPCONV_API int64_t spconv_layer_norm_bwd_workspace(int64_t rows, int C);
+
+/* Gradients of spconv_layer_norm_fwd:
+ *   g = dout where the ReLU let it through (y > 0), else 0; g = dout without a ReLU
+ *   xh = (x - m) * r, h = g * weight, dx = r * (h - mean(h) - xh * mean(h * xh)),
+ *   dweight = sum over rows of g * xh, dbias = sum over rows of g, dresidual = g
+ *   x or kept_x      the norm's input, or its checkpoint: exactly one
+ *   y or kept_y      the output, or its checkpoint, of a norm with a ReLU; both NULL: no ReLU
+ *   stats            what the forward pass left
+ *   dx               device [rows][C], fully overwritten; may be dout
+ *   dresidual        device [rows][C], or NULL
+ *   dweight, dbias   device fp32 [C], fully overwritten, or both NULL
+ *   workspace        device, at least spconv_layer_norm_bwd_workspace(rows, C) bytes, 16-byte aligned, for this call alone until it is
+ *                    done; unused (may be NULL) without dweight
+ * Sums are fp32 in a fixed order: the same call gives the same bits.  rows = 0 gives zero dweight and dbias.  EINVAL as above. */
+SPCONV_API int spconv_layer_norm_bwd(const void* dout, const void* x_or_null, const spconv_q8* kept_x_or_null,
+                                     const void* y_or_null, const spconv_q8* kept_y_or_null, const float* weight_or_null,
+                                     const float* stats, int64_t rows, int C, spconv_dtype dtype, void* dx,
+                                     void* dresidual_or_null, float* dweight_or_null, float* dbias_or_null, void* workspace,
+                                     int64_t workspace_bytes, void* stream);
+
 /* Picks the configuration of the design space of Section 4.1 (dataflow: implicit
  * GEMM or fetch-on-demand; number of splits, sorted or not; tile sizes) with the
  * lowest measured time for op on

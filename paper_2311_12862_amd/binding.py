@@ -45,6 +45,11 @@ class LayerShape(C.Structure):
     _fields_ = [("c_in", C.c_int32), ("c_out", C.c_int32)]
 
 
+class Q8(C.Structure):
+    """Mirror of spconv_q8."""
+    _fields_ = [("data", C.c_void_p), ("exps", C.c_void_p)]
+
+
 class LaunchInfo(C.Structure):
     """Mirror of spconv_launch_info."""
     _fields_ = [("kernel", C.c_int32), ("parts", C.c_int32), ("sorted", C.c_int32), ("tile_m", C.c_int32),
@@ -99,6 +104,15 @@ def load_library():
                                     C.POINTER(C.c_float), vp]),
         "spconv_ew": (i32, [i32, vp, vp, vp, i64, i32, vp]),
         "spconv_copy_cols": (i32, [vp, i32, i32, vp, i32, i32, i32, i64, i32, vp]),
+        "spconv_q8_pack": (i32, [vp, i64, i32, i32, C.POINTER(Q8), vp]),
+        "spconv_q8_unpack": (i32, [C.POINTER(Q8), i64, i32, i32, vp, vp]),
+        "spconv_relu_bwd_q8": (i32, [vp, C.POINTER(Q8), vp, i64, i32, vp]),
+        "spconv_wgrad_q8": (i32, [C.POINTER(Q8), vp, vp, i32, i32, i32, cfgp, vp, vp]),
+        "spconv_layer_norm_fwd": (i32, [vp, vp, vp, vp, C.c_float, i32, i64, i32, i32, vp, vp, C.POINTER(Q8),
+                                        C.POINTER(Q8), vp]),
+        "spconv_layer_norm_bwd_workspace": (i64, [i64, i32]),
+        "spconv_layer_norm_bwd": (i32, [vp, vp, C.POINTER(Q8), vp, C.POINTER(Q8), vp, vp, i64, i32, i32, vp, vp, vp, vp,
+                                        vp, i64, vp]),
         "spconv_set_allocator": (i32, [vp, vp, vp]),
         "spconv_describe_launch": (i32, [i32, i64, i64, i32, i32, i32, cfgp, i32, C.POINTER(LaunchInfo)]),
         "spconv_measure_peaks": (i32, [C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
@@ -361,7 +375,10 @@ def dgrad(dout, weights, kmap: KMap, cfg: Config | None = None, out=None, stream
 
 
 def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=None):
-    """spconv_wgrad: feats [n_in, C_in], dout [n_out, C_out] -> dweights fp32 [K^3, C_in, C_out]."""
+    """spconv_wgrad: feats [n_in, C_in], dout [n_out, C_out] -> dweights fp32 [K^3, C_in, C_out].
+    feats may be a Checkpoint of the layer's input (spconv_wgrad_q8)."""
+    if isinstance(feats, Checkpoint):
+        return _wgrad_q8(feats, dout, kmap, cfg, out, stream)
     dt = _conv_args(feats, dout, kmap, kmap.n_in)
     if dout.ndim != 2 or dout.shape[0] != kmap.n_out:
         raise SpconvError(-5, "dout rows do not fit the kmap")
@@ -374,6 +391,23 @@ def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=N
                                _stream(stream))
     if status:
         _check(status, "spconv_wgrad")
+    return out
+
+
+def _wgrad_q8(kept, dout, kmap, cfg, out, stream):
+    _dev_tensor(dout)
+    dt = _dtype_number(dout)
+    if dout.ndim != 2 or dout.shape[0] != kmap.n_out or kept.rows != kmap.n_in:
+        raise SpconvError(-5, f"rows of the checkpoint ({kept.rows}) or of dout {tuple(dout.shape)} do not fit the kmap "
+                              f"({kmap.n_in} in, {kmap.n_out} out)")
+    with _on(dout, kept.data):
+        c_in, c_out = kept.channels, dout.shape[1]
+        if out is None:
+            out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
+        else:
+            _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
+        _check(load_library().spconv_wgrad_q8(C.byref(kept.ref()), _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg),
+                                              _ptr(out), _stream(stream)), "spconv_wgrad_q8")
     return out
 
 
@@ -421,8 +455,11 @@ EW_RELU, EW_ADD, EW_ADD_RELU, EW_RELU_BWD = 0, 1, 2, 3
 
 
 def ew(op: int, a, b=None, out=None, stream=None):
-    """spconv_ew: element-wise glue (see include/spconv.h); out defaults to a new tensor like a."""
+    """spconv_ew: element-wise glue (see include/spconv.h); out defaults to a new tensor like a.
+    For EW_RELU_BWD, b may be a Checkpoint of the ReLU's output (spconv_relu_bwd_q8)."""
     _dev_tensor(a)
+    if isinstance(b, Checkpoint):
+        return _relu_bwd_q8(op, a, b, out, stream)
     if b is not None:
         _dev_tensor(b, a.dtype)
         if b.shape != a.shape:
@@ -435,6 +472,23 @@ def ew(op: int, a, b=None, out=None, stream=None):
     return out
 
 
+def _relu_bwd_q8(op, a, kept, out, stream):
+    if op != EW_RELU_BWD:
+        raise ValueError("a Checkpoint stands for the output of EW_RELU_BWD only")
+    dt = _dtype_number(a)
+    if tuple(a.shape) != (kept.rows, kept.channels):
+        raise ValueError("shape mismatch")
+    if out is None:
+        out = torch.empty_like(a)
+    else:
+        _out_tensor(out, a.shape, a.dtype, a)
+    with _on(a, kept.data):
+        status = load_library().spconv_relu_bwd_q8(_ptr(a), C.byref(kept.ref()), _ptr(out), a.numel(), dt, _stream(stream))
+    if status:
+        _check(status, "spconv_relu_bwd_q8")
+    return out
+
+
 def copy_cols(src, src_off: int, dst, dst_off: int, cols: int, stream=None):
     """spconv_copy_cols on two [rows, ld] tensors."""
     _dev_tensor(src)
@@ -444,3 +498,194 @@ def copy_cols(src, src_off: int, dst, dst_off: int, cols: int, stream=None):
     _check(load_library().spconv_copy_cols(_ptr(src), src.shape[1], src_off, _ptr(dst), dst.shape[1], dst_off, cols,
                                            src.shape[0], _DTYPES[src.dtype], _stream(stream)), "spconv_copy_cols")
     return dst
+
+
+# ---- layer norm and 8-bit checkpoints ------------------------------------------------------------
+
+def _dtype_number(t):
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return dt
+
+
+class _Here:
+    """The tensors are on the current device: nothing to switch."""
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        return False
+
+
+_HERE = _Here()
+
+
+def _on(t, *others):
+    """The device of t for the length of a call (its streams, its launches); the others have to be on it as well."""
+    for o in others:
+        if o is not None and o.device != t.device:
+            raise ValueError(f"tensors on {t.device} and {o.device}")
+    return _HERE if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+class Checkpoint:
+    """An activation [rows, channels] kept in 8 bits (spconv_q8): data int8 [rows, channels], exps uint8
+    [rows, ceil(channels / 32)].  What a backward pass reads an activation for takes a Checkpoint in its place: `wgrad`,
+    `layer_norm_bwd` and the gradient through a ReLU, `ew(EW_RELU_BWD, ...)`."""
+    __slots__ = ("data", "exps")
+
+    def __init__(self, data, exps):
+        _dev_tensor(data, torch.int8)
+        _dev_tensor(exps, torch.uint8)
+        if data.ndim != 2 or exps.ndim != 2 or tuple(exps.shape) != (data.shape[0], -(-data.shape[1] // 32)):
+            raise ValueError(f"data is {tuple(data.shape)}, exps {tuple(exps.shape)}: expected [rows, C] and [rows, ceil(C / 32)]")
+        if data.device != exps.device:
+            raise ValueError(f"tensors on {data.device} and {exps.device}")
+        self.data, self.exps = data, exps
+
+    @classmethod
+    def empty(cls, rows: int, channels: int, device=_CUDA) -> "Checkpoint":
+        return cls(torch.empty((rows, channels), dtype=torch.int8, device=device),
+                   torch.empty((rows, -(-channels // 32)), dtype=torch.uint8, device=device))
+
+    @property
+    def rows(self) -> int:
+        return self.data.shape[0]
+
+    @property
+    def channels(self) -> int:
+        return self.data.shape[1]
+
+    @property
+    def device(self):
+        return self.data.device
+
+    def ref(self) -> Q8:
+        return Q8(_ptr(self.data), _ptr(self.exps))
+
+
+def _rows_tensor(t, dtype=None):
+    _dev_tensor(t, dtype)
+    if t.ndim != 2:
+        raise ValueError(f"expected a tensor [rows, channels], got {tuple(t.shape)}")
+    return t
+
+
+def _kept_like(kept, t):
+    if not isinstance(kept, Checkpoint):
+        raise ValueError(f"expected a Checkpoint, got {type(kept).__name__}")
+    if (kept.rows, kept.channels) != tuple(t.shape):
+        raise SpconvError(-5, f"the checkpoint is {(kept.rows, kept.channels)}, the tensor {tuple(t.shape)}")
+    if kept.device != t.device:
+        raise ValueError(f"tensors on {t.device} and {kept.device}")
+    return kept
+
+
+def _per_channel(t, like):
+    if t is not None:
+        _dev_tensor(t, torch.float32)
+        if tuple(t.shape) != (like.shape[1],):
+            raise SpconvError(-5, f"expected [{like.shape[1]}] values per channel, got {tuple(t.shape)}")
+    return t
+
+
+def _byref(kept):
+    return None if kept is None else C.byref(kept.ref())
+
+
+def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
+    """spconv_q8_pack: the 8-bit checkpoint of x [rows, channels]."""
+    _rows_tensor(x)
+    dt = _dtype_number(x)
+    if out is None:
+        out = Checkpoint.empty(x.shape[0], x.shape[1], x.device)
+    else:
+        _kept_like(out, x)
+    with _on(x):
+        _check(load_library().spconv_q8_pack(_ptr(x), x.shape[0], x.shape[1], dt, C.byref(out.ref()), _stream(stream)),
+               "spconv_q8_pack")
+    return out
+
+
+def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
+    """spconv_q8_unpack: the values that a checkpoint stands for, as a tensor of dtype."""
+    if out is None:
+        out = torch.empty((kept.rows, kept.channels), dtype=dtype, device=kept.device)
+    else:
+        _out_tensor(out, (kept.rows, kept.channels), dtype, kept.data)
+    with _on(out):
+        _check(load_library().spconv_q8_unpack(C.byref(kept.ref()), kept.rows, kept.channels, _dtype_number(out), _ptr(out),
+                                               _stream(stream)), "spconv_q8_unpack")
+    return out
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = False, residual=None, out=None,
+                   keep_x: Checkpoint | None = None, keep_y: Checkpoint | None = None, stream=None):
+    """spconv_layer_norm_fwd: (y, stats) with y = act(norm(x) * weight + bias + residual), x and y [rows, channels],
+    weight and bias fp32 [channels], stats fp32 [rows, 2] = (mean, 1 / std) for layer_norm_bwd.  keep_x and keep_y are
+    filled with checkpoints of x and y in the same pass."""
+    _rows_tensor(x)
+    dt = _dtype_number(x)
+    _per_channel(weight, x)
+    _per_channel(bias, x)
+    if residual is not None:
+        _out_tensor(residual, x.shape, x.dtype, x)
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _out_tensor(out, x.shape, x.dtype, x)
+    for kept in (keep_x, keep_y):
+        if kept is not None:
+            _kept_like(kept, x)
+    with _on(x, weight, bias):
+        stats = torch.empty((x.shape[0], 2), dtype=torch.float32, device=x.device)
+        _check(load_library().spconv_layer_norm_fwd(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), eps, int(bool(relu)),
+                                                    x.shape[0], x.shape[1], dt, _ptr(out), _ptr(stats), _byref(keep_x),
+                                                    _byref(keep_y), _stream(stream)), "spconv_layer_norm_fwd")
+    return out, stats
+
+
+def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = False, affine: bool = True, stream=None):
+    """spconv_layer_norm_bwd: (dx, dweight, dbias, dresidual) for a layer_norm_fwd that left stats.  x: its input or the
+    Checkpoint of it; gate: its output or the Checkpoint of it where it had a ReLU.  dweight and dbias are fp32 [channels]
+    (None for affine=False), dresidual is None unless residual is set."""
+    _rows_tensor(dout)
+    dt = _dtype_number(dout)
+    rows, channels = dout.shape
+    _dev_tensor(stats, torch.float32)
+    if tuple(stats.shape) != (rows, 2):
+        raise SpconvError(-5, f"stats are {tuple(stats.shape)}, expected {(rows, 2)}")
+    _per_channel(weight, dout)
+    kept_x = _kept_like(x, dout) if isinstance(x, Checkpoint) else None
+    kept_y = _kept_like(gate, dout) if isinstance(gate, Checkpoint) else None
+    for t in (x, gate):
+        if t is not None and not isinstance(t, Checkpoint):
+            _out_tensor(t, dout.shape, dout.dtype, dout)
+    if x is None:
+        raise ValueError("x is the norm's input or its Checkpoint")
+    lib = load_library()
+    with _on(dout, stats, weight):
+        dx = torch.empty_like(dout)
+        dres = torch.empty_like(dout) if residual else None
+        dweight = dbias = workspace = None
+        need = 0
+        if affine:
+            need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
+            if need < 0:
+                _check(need, "spconv_layer_norm_bwd_workspace")
+            sums = torch.empty((2, channels), dtype=torch.float32, device=dout.device)
+            dweight, dbias = sums[0], sums[1]
+            workspace = torch.empty((need,), dtype=torch.uint8, device=dout.device)
+        st = _stream(stream)
+        status = lib.spconv_layer_norm_bwd(_ptr(dout), None if kept_x else _ptr(x), _byref(kept_x),
+                                           None if kept_y or gate is None else _ptr(gate), _byref(kept_y), _ptr(weight),
+                                           _ptr(stats), rows, channels, dt, _ptr(dx), _ptr(dres), _ptr(dweight), _ptr(dbias),
+                                           _ptr(workspace), need, st)
+        if status:
+            _check(status, "spconv_layer_norm_bwd")
+        if workspace is not None and stream is not None and st != _stream(None):
+            # the caller's stream is still to use it when this function lets go of it
+            workspace.record_stream(torch.cuda.ExternalStream(st, device=dout.device))
+    return dx, dweight, dbias, dres

@@ -739,6 +739,20 @@ SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km
   return wgrad_run(km, *pl, c.wgrad_pairs, feats, dout, C_in, C_out, dtype, dweights, st);
 }
 
+SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
+                               const spconv_config* cfg, float* dweights, void* stream) {
+  StreamScope scope((hipStream_t)stream);
+  if (!km || !dtype_ok(dtype) || !dweights || !kept) return SPCONV_EINVAL;
+  SPC_TRY(check_channels(C_in, C_out, dtype));
+  if (km->n_out > 0 && km->n_in > 0 && (!kept->data || !kept->exps || !dout)) return SPCONV_EINVAL;
+  hipStream_t st = (hipStream_t)stream;
+  spconv_config c;
+  SPC_TRY(resolve_config(cfg, dtype, &c));
+  SPC_TRY(km->unpacked.reserve((size_t)km->n_in * C_in * (dtype == SPCONV_F32 ? 4 : 2)));
+  if (km->n_in > 0) SPC_TRY(q8_unpack(kept, km->n_in, C_in, dtype, km->unpacked.p, st));
+  return spconv_wgrad(km->unpacked.p, dout, km, C_in, C_out, dtype, cfg, dweights, stream);
+}
+
 }  // extern "C"
 
 namespace {

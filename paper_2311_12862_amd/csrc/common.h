@@ -161,6 +161,7 @@ struct spconv_kmap {
   // the parts of a split.  Offset k of the whole map is offset k % 25 of plane k / 25.
   std::vector<std::unique_ptr<spconv_kmap>> groups;
   spc::DevBuf scratch;    // split partial sums / wgrad partial tiles
+  spc::DevBuf unpacked;   // the tensor of a checkpoint that wgrad reads
   // build whose status was not read yet: the pinned block the probe kernel publishes flags and
   // pair count to, with the event that marks the probe's completion
   void* pending_host = nullptr;
@@ -256,6 +257,15 @@ int item_plan_get(spconv_kmap* km, int64_t target, hipStream_t st, ItemPlan** ou
 
 // ---- order.hip: fills perm, maps and tilemask of a one-part plan in the library's own order
 int order_rows(const SideMap& side, int V, IgemmPlan& p, hipStream_t st);
+
+// ---- norm.hip, checkpoint.hip: tensors of rows of channels
+constexpr int kRowMaxChannels = 4096;
+constexpr int64_t kRowMaxElements = (int64_t)1 << 40;
+inline bool row_shape_ok(int64_t rows, int C) {
+  return rows >= 0 && C >= 1 && C <= kRowMaxChannels && rows <= kRowMaxElements / C;
+}
+inline bool dtype_known(int d) { return d == SPCONV_F32 || d == SPCONV_F16 || d == SPCONV_BF16; }
+int q8_unpack(const spconv_q8* from, int64_t rows, int C, spconv_dtype dtype, void* out, hipStream_t st);
 
 // ---- igemm.hip
 struct IgemmArgs {
