@@ -395,19 +395,24 @@ def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=N
 
 
 def _wgrad_q8(kept, dout, kmap, cfg, out, stream):
-    _dev_tensor(dout)
-    dt = _dtype_number(dout)
-    if dout.ndim != 2 or dout.shape[0] != kmap.n_out or kept.rows != kmap.n_in:
+    dt = _row_args(dout)
+    if dout.shape[0] != kmap.n_out or kept.rows != kmap.n_in:
         raise SpconvError(-5, f"rows of the checkpoint ({kept.rows}) or of dout {tuple(dout.shape)} do not fit the kmap "
                               f"({kmap.n_in} in, {kmap.n_out} out)")
-    with _on(dout, kept.data):
-        c_in, c_out = kept.channels, dout.shape[1]
-        if out is None:
-            out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
-        else:
-            _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
-        _check(load_library().spconv_wgrad_q8(C.byref(kept.ref()), _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg),
-                                              _ptr(out), _stream(stream)), "spconv_wgrad_q8")
+    if kept.get_device() != dout.get_device():
+        raise ValueError(f"tensors on {dout.device} and {kept.device}")
+    if dout.get_device() != _device_now():
+        with torch.cuda.device(dout.device):
+            return _wgrad_q8(kept, dout, kmap, cfg, out, stream)
+    c_in, c_out = kept.channels, dout.shape[1]
+    if out is None:
+        out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
+    else:
+        _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
+    status = _LIB.spconv_wgrad_q8(C.byref(kept.ref), _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
+                                  _stream(stream))
+    if status:
+        _check(status, "spconv_wgrad_q8")
     return out
 
 
@@ -457,9 +462,9 @@ EW_RELU, EW_ADD, EW_ADD_RELU, EW_RELU_BWD = 0, 1, 2, 3
 def ew(op: int, a, b=None, out=None, stream=None):
     """spconv_ew: element-wise glue (see include/spconv.h); out defaults to a new tensor like a.
     For EW_RELU_BWD, b may be a Checkpoint of the ReLU's output (spconv_relu_bwd_q8)."""
-    _dev_tensor(a)
     if isinstance(b, Checkpoint):
         return _relu_bwd_q8(op, a, b, out, stream)
+    _dev_tensor(a)
     if b is not None:
         _dev_tensor(b, a.dtype)
         if b.shape != a.shape:
@@ -475,15 +480,19 @@ def ew(op: int, a, b=None, out=None, stream=None):
 def _relu_bwd_q8(op, a, kept, out, stream):
     if op != EW_RELU_BWD:
         raise ValueError("a Checkpoint stands for the output of EW_RELU_BWD only")
-    dt = _dtype_number(a)
-    if tuple(a.shape) != (kept.rows, kept.channels):
+    dt = _row_args(a)
+    if a.shape != (kept.rows, kept.channels):
         raise ValueError("shape mismatch")
+    if kept.get_device() != a.get_device():
+        raise ValueError(f"tensors on {a.device} and {kept.device}")
+    if a.get_device() != _device_now():
+        with torch.cuda.device(a.device):
+            return _relu_bwd_q8(op, a, kept, out, stream)
     if out is None:
         out = torch.empty_like(a)
     else:
         _out_tensor(out, a.shape, a.dtype, a)
-    with _on(a, kept.data):
-        status = load_library().spconv_relu_bwd_q8(_ptr(a), C.byref(kept.ref()), _ptr(out), a.numel(), dt, _stream(stream))
+    status = (_LIB or load_library()).spconv_relu_bwd_q8(_ptr(a), C.byref(kept.ref), _ptr(out), a.numel(), dt, _stream(stream))
     if status:
         _check(status, "spconv_relu_bwd_q8")
     return out
@@ -501,123 +510,141 @@ def copy_cols(src, src_off: int, dst, dst_off: int, cols: int, stream=None):
 
 
 # ---- layer norm and 8-bit checkpoints ------------------------------------------------------------
+# A call of these takes 6 to 14 us on the host (two of each three go to torch's allocations and the launches), more than many of
+# their kernels: checks read a tensor's attributes once, and the device is switched only where it is another one.
 
-def _dtype_number(t):
-    dt = _DTYPES.get(t.dtype)
-    if dt is None:
-        raise ValueError(f"unsupported dtype {t.dtype}")
+def _device_now():
+    """Number of the current device (a look-up, as in _current_stream)."""
+    global _device_now
+    torch.cuda.current_device()   # (initialises the device if nothing has yet)
+    _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _device_now()
+
+
+def _row_args(x):
+    """The data type's number of a tensor [rows, channels]; what is none raises."""
+    dt = _DTYPES.get(x.dtype)
+    if dt is None or x.ndim != 2 or not x.is_cuda or not x.is_contiguous():
+        _dev_tensor(x)
+        raise ValueError(f"expected a tensor [rows, channels] of {', '.join(map(str, _DTYPES))}, got {tuple(x.shape)} of {x.dtype}")
     return dt
 
 
-class _Here:
-    """The tensors are on the current device: nothing to switch."""
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *_):
-        return False
+def _like(t, x):
+    """t: a tensor that a call takes or fills beside x, of the same shape, type and device."""
+    if t.dtype is not x.dtype or t.shape != x.shape or not t.is_contiguous() or t.get_device() != x.get_device():
+        _out_tensor(t, x.shape, x.dtype, x)
+    return t
 
 
-_HERE = _Here()
+def _kept_like(kept, x):
+    if not isinstance(kept, Checkpoint):
+        raise ValueError(f"expected a Checkpoint, got {type(kept).__name__}")
+    if x.shape != (kept.rows, kept.channels):
+        raise SpconvError(-5, f"the checkpoint is {(kept.rows, kept.channels)}, the tensor {tuple(x.shape)}")
+    if kept.get_device() != x.get_device():
+        raise ValueError(f"tensors on {x.device} and {kept.device}")
+    return C.byref(kept.ref)
 
 
-def _on(t, *others):
-    """The device of t for the length of a call (its streams, its launches); the others have to be on it as well."""
-    for o in others:
-        if o is not None and o.device != t.device:
-            raise ValueError(f"tensors on {t.device} and {o.device}")
-    return _HERE if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+def _floats(t, shape, x):
+    """Address of fp32 values that a call reads beside x."""
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != x.get_device():
+        _dev_tensor(t, torch.float32)
+        if t.shape != shape:
+            raise SpconvError(-5, f"expected fp32 values {shape}, got {tuple(t.shape)}")
+        raise ValueError(f"tensors on {x.device} and {t.device}")
+    return t.data_ptr()
 
 
 class Checkpoint:
     """An activation [rows, channels] kept in 8 bits (spconv_q8): data int8 [rows, channels], exps uint8
     [rows, ceil(channels / 32)].  What a backward pass reads an activation for takes a Checkpoint in its place: `wgrad`,
     `layer_norm_bwd` and the gradient through a ReLU, `ew(EW_RELU_BWD, ...)`."""
-    __slots__ = ("data", "exps")
+    __slots__ = ("rows", "channels", "ref", "_data", "_exps")
 
     def __init__(self, data, exps):
         _dev_tensor(data, torch.int8)
         _dev_tensor(exps, torch.uint8)
-        if data.ndim != 2 or exps.ndim != 2 or tuple(exps.shape) != (data.shape[0], -(-data.shape[1] // 32)):
+        if data.ndim != 2 or exps.ndim != 2 or exps.shape != (data.shape[0], -(-data.shape[1] // 32)):
             raise ValueError(f"data is {tuple(data.shape)}, exps {tuple(exps.shape)}: expected [rows, C] and [rows, ceil(C / 32)]")
         if data.device != exps.device:
             raise ValueError(f"tensors on {data.device} and {exps.device}")
-        self.data, self.exps = data, exps
+        self.rows, self.channels = data.shape
+        self._data, self._exps = data, exps
+        self.ref = Q8(_ptr(data), _ptr(exps))
 
     @classmethod
     def empty(cls, rows: int, channels: int, device=_CUDA) -> "Checkpoint":
-        return cls(torch.empty((rows, channels), dtype=torch.int8, device=device),
-                   torch.empty((rows, -(-channels // 32)), dtype=torch.uint8, device=device))
+        """Room for the checkpoint of a tensor [rows, channels] (one allocation: data, then exps)."""
+        if rows < 0 or channels < 1:
+            raise ValueError(f"no tensor is [{rows}, {channels}]")
+        self = cls.__new__(cls)
+        self.rows, self.channels = rows, channels
+        at = (rows * channels + 15) // 16 * 16
+        self._data = torch.empty((at + rows * (-(-channels // 32)),), dtype=torch.int8, device=device)
+        self._exps = at
+        base = self._data.data_ptr()
+        if base == 0 and rows:
+            raise ValueError("expected a contiguous device tensor")
+        self.ref = Q8(base or None, base + at or None)
+        return self
+
+    def _views(self):
+        if not isinstance(self._exps, torch.Tensor):
+            room, at = self._data, self._exps
+            self._exps = room[at:].view(torch.uint8).view(self.rows, -1) if self.rows else room.view(torch.uint8).view(0, -(-self.channels // 32))
+            self._data = room[:self.rows * self.channels].view(self.rows, self.channels)
 
     @property
-    def rows(self) -> int:
-        return self.data.shape[0]
+    def data(self):
+        self._views()
+        return self._data
 
     @property
-    def channels(self) -> int:
-        return self.data.shape[1]
+    def exps(self):
+        self._views()
+        return self._exps
 
     @property
     def device(self):
-        return self.data.device
+        return self._data.device
 
-    def ref(self) -> Q8:
-        return Q8(_ptr(self.data), _ptr(self.exps))
-
-
-def _rows_tensor(t, dtype=None):
-    _dev_tensor(t, dtype)
-    if t.ndim != 2:
-        raise ValueError(f"expected a tensor [rows, channels], got {tuple(t.shape)}")
-    return t
-
-
-def _kept_like(kept, t):
-    if not isinstance(kept, Checkpoint):
-        raise ValueError(f"expected a Checkpoint, got {type(kept).__name__}")
-    if (kept.rows, kept.channels) != tuple(t.shape):
-        raise SpconvError(-5, f"the checkpoint is {(kept.rows, kept.channels)}, the tensor {tuple(t.shape)}")
-    if kept.device != t.device:
-        raise ValueError(f"tensors on {t.device} and {kept.device}")
-    return kept
-
-
-def _per_channel(t, like):
-    if t is not None:
-        _dev_tensor(t, torch.float32)
-        if tuple(t.shape) != (like.shape[1],):
-            raise SpconvError(-5, f"expected [{like.shape[1]}] values per channel, got {tuple(t.shape)}")
-    return t
-
-
-def _byref(kept):
-    return None if kept is None else C.byref(kept.ref())
+    def get_device(self) -> int:
+        return self._data.get_device()
 
 
 def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """spconv_q8_pack: the 8-bit checkpoint of x [rows, channels]."""
-    _rows_tensor(x)
-    dt = _dtype_number(x)
+    dt = _row_args(x)
+    if x.get_device() != _device_now():
+        with torch.cuda.device(x.device):
+            return q8_pack(x, out, stream)
+    rows, channels = x.shape
     if out is None:
-        out = Checkpoint.empty(x.shape[0], x.shape[1], x.device)
-    else:
-        _kept_like(out, x)
-    with _on(x):
-        _check(load_library().spconv_q8_pack(_ptr(x), x.shape[0], x.shape[1], dt, C.byref(out.ref()), _stream(stream)),
-               "spconv_q8_pack")
+        out = Checkpoint.empty(rows, channels, x.device)
+    status = (_LIB or load_library()).spconv_q8_pack(_ptr(x), rows, channels, dt, _kept_like(out, x), _stream(stream))
+    if status:
+        _check(status, "spconv_q8_pack")
     return out
 
 
 def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
     """spconv_q8_unpack: the values that a checkpoint stands for, as a tensor of dtype."""
+    dt = _DTYPES.get(dtype)
+    if dt is None:
+        raise ValueError(f"unsupported dtype {dtype}")
+    if kept.get_device() != _device_now():
+        with torch.cuda.device(kept.device):
+            return q8_unpack(kept, dtype, out, stream)
+    shape = (kept.rows, kept.channels)
     if out is None:
-        out = torch.empty((kept.rows, kept.channels), dtype=dtype, device=kept.device)
+        out = torch.empty(shape, dtype=dtype, device=kept.device)
     else:
-        _out_tensor(out, (kept.rows, kept.channels), dtype, kept.data)
-    with _on(out):
-        _check(load_library().spconv_q8_unpack(C.byref(kept.ref()), kept.rows, kept.channels, _dtype_number(out), _ptr(out),
-                                               _stream(stream)), "spconv_q8_unpack")
+        _out_tensor(out, shape, dtype, kept)
+    status = (_LIB or load_library()).spconv_q8_unpack(C.byref(kept.ref), *shape, dt, _ptr(out), _stream(stream))
+    if status:
+        _check(status, "spconv_q8_unpack")
     return out
 
 
@@ -626,24 +653,24 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     """spconv_layer_norm_fwd: (y, stats) with y = act(norm(x) * weight + bias + residual), x and y [rows, channels],
     weight and bias fp32 [channels], stats fp32 [rows, 2] = (mean, 1 / std) for layer_norm_bwd.  keep_x and keep_y are
     filled with checkpoints of x and y in the same pass."""
-    _rows_tensor(x)
-    dt = _dtype_number(x)
-    _per_channel(weight, x)
-    _per_channel(bias, x)
+    dt = _row_args(x)
+    if x.get_device() != _device_now():
+        with torch.cuda.device(x.device):
+            return layer_norm_fwd(x, weight, bias, eps, relu, residual, out, keep_x, keep_y, stream)
+    rows, channels = x.shape
+    w = None if weight is None else _floats(weight, (channels,), x)
+    b = None if bias is None else _floats(bias, (channels,), x)
     if residual is not None:
-        _out_tensor(residual, x.shape, x.dtype, x)
-    if out is None:
-        out = torch.empty_like(x)
-    else:
-        _out_tensor(out, x.shape, x.dtype, x)
-    for kept in (keep_x, keep_y):
-        if kept is not None:
-            _kept_like(kept, x)
-    with _on(x, weight, bias):
-        stats = torch.empty((x.shape[0], 2), dtype=torch.float32, device=x.device)
-        _check(load_library().spconv_layer_norm_fwd(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), eps, int(bool(relu)),
-                                                    x.shape[0], x.shape[1], dt, _ptr(out), _ptr(stats), _byref(keep_x),
-                                                    _byref(keep_y), _stream(stream)), "spconv_layer_norm_fwd")
+        _like(residual, x)
+    kept_x = None if keep_x is None else _kept_like(keep_x, x)
+    kept_y = None if keep_y is None else _kept_like(keep_y, x)
+    out = torch.empty_like(x) if out is None else _like(out, x)
+    stats = x.new_empty((rows, 2), dtype=torch.float32)
+    status = (_LIB or load_library()).spconv_layer_norm_fwd(
+        _ptr(x), None if residual is None else _ptr(residual), w, b, eps, 1 if relu else 0, rows, channels, dt, _ptr(out),
+        _ptr(stats), kept_x, kept_y, _stream(stream))
+    if status:
+        _check(status, "spconv_layer_norm_fwd")
     return out, stats
 
 
@@ -651,41 +678,43 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
     """spconv_layer_norm_bwd: (dx, dweight, dbias, dresidual) for a layer_norm_fwd that left stats.  x: its input or the
     Checkpoint of it; gate: its output or the Checkpoint of it where it had a ReLU.  dweight and dbias are fp32 [channels]
     (None for affine=False), dresidual is None unless residual is set."""
-    _rows_tensor(dout)
-    dt = _dtype_number(dout)
+    dt = _row_args(dout)
+    if dout.get_device() != _device_now():
+        with torch.cuda.device(dout.device):
+            return layer_norm_bwd(dout, x, stats, weight, gate, residual, affine, stream)
     rows, channels = dout.shape
-    _dev_tensor(stats, torch.float32)
-    if tuple(stats.shape) != (rows, 2):
-        raise SpconvError(-5, f"stats are {tuple(stats.shape)}, expected {(rows, 2)}")
-    _per_channel(weight, dout)
-    kept_x = _kept_like(x, dout) if isinstance(x, Checkpoint) else None
-    kept_y = _kept_like(gate, dout) if isinstance(gate, Checkpoint) else None
-    for t in (x, gate):
-        if t is not None and not isinstance(t, Checkpoint):
-            _out_tensor(t, dout.shape, dout.dtype, dout)
+    st_ptr = _floats(stats, (rows, 2), dout)
+    w = None if weight is None else _floats(weight, (channels,), dout)
+    x_ptr = kept_x = y_ptr = kept_y = None
     if x is None:
         raise ValueError("x is the norm's input or its Checkpoint")
-    lib = load_library()
-    with _on(dout, stats, weight):
-        dx = torch.empty_like(dout)
-        dres = torch.empty_like(dout) if residual else None
-        dweight = dbias = workspace = None
-        need = 0
-        if affine:
-            need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
-            if need < 0:
-                _check(need, "spconv_layer_norm_bwd_workspace")
-            sums = torch.empty((2, channels), dtype=torch.float32, device=dout.device)
-            dweight, dbias = sums[0], sums[1]
-            workspace = torch.empty((need,), dtype=torch.uint8, device=dout.device)
-        st = _stream(stream)
-        status = lib.spconv_layer_norm_bwd(_ptr(dout), None if kept_x else _ptr(x), _byref(kept_x),
-                                           None if kept_y or gate is None else _ptr(gate), _byref(kept_y), _ptr(weight),
-                                           _ptr(stats), rows, channels, dt, _ptr(dx), _ptr(dres), _ptr(dweight), _ptr(dbias),
-                                           _ptr(workspace), need, st)
-        if status:
-            _check(status, "spconv_layer_norm_bwd")
-        if workspace is not None and stream is not None and st != _stream(None):
-            # the caller's stream is still to use it when this function lets go of it
-            workspace.record_stream(torch.cuda.ExternalStream(st, device=dout.device))
+    if isinstance(x, Checkpoint):
+        kept_x = _kept_like(x, dout)
+    else:
+        x_ptr = _ptr(_like(x, dout))
+    if isinstance(gate, Checkpoint):
+        kept_y = _kept_like(gate, dout)
+    elif gate is not None:
+        y_ptr = _ptr(_like(gate, dout))
+    lib = _LIB or load_library()
+    dx = torch.empty_like(dout)
+    dres = torch.empty_like(dout) if residual else None
+    dweight = dbias = dw_ptr = db_ptr = workspace = ws_ptr = None
+    need = 0
+    if affine:
+        need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
+        if need < 0:
+            _check(need, "spconv_layer_norm_bwd_workspace")
+        dweight = dout.new_empty((channels,), dtype=torch.float32)
+        dbias = dout.new_empty((channels,), dtype=torch.float32)
+        workspace = dout.new_empty((need,), dtype=torch.int8)
+        dw_ptr, db_ptr, ws_ptr = dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr()
+    st = _stream(stream)
+    status = lib.spconv_layer_norm_bwd(_ptr(dout), x_ptr, kept_x, y_ptr, kept_y, w, st_ptr if rows else None, rows, channels, dt,
+                                       _ptr(dx), None if dres is None else _ptr(dres), dw_ptr, db_ptr, ws_ptr, need, st)
+    if status:
+        _check(status, "spconv_layer_norm_bwd")
+    if workspace is not None and stream is not None and st != _stream(None):
+        # the caller's stream is still to use it when this function lets go of it
+        workspace.record_stream(torch.cuda.ExternalStream(st, device=dout.device))
     return dx, dweight, dbias, dres

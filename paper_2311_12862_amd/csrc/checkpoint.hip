@@ -8,89 +8,106 @@
 namespace spc {
 namespace {
 
-// A group of 32 / W lanes takes one block of a row.
-template <typename T, int W>
-__global__ void __launch_bounds__(256) k_q8_pack(const T* __restrict__ x, Q8Ref to, long long blocks, int C, int nb) {
-  constexpr int G = kQ8Block / W;
-  const long long stride = (long long)gridDim.x * (256 / G);
-  const int lane = threadIdx.x % G;
-  for (long long i = (long long)blockIdx.x * (256 / G) + threadIdx.x / G; i < blocks; i += stride) {
-    const long long r = i / nb;
-    const int col = (int)(i - r * nb) * kQ8Block + lane * W;
-    const bool live = col < C;
-    float v[W] = {};
-    if (live) Chunk<T, W>::load(x, r * C + col, v);
-    q8_keep<G, W>(to, r, C, nb, col, live, v);
+// Rows of C channels, a group of L lanes each; 256 / L rows of a workgroup, whose first is the same for all its lanes (addresses are a
+// scalar base and 32 bits per lane).
+template <typename T, int L, int NV, bool TAIL>
+__global__ void __launch_bounds__(256) k_q8_pack(const T* __restrict__ x, Q8Ref to, long long rows, int C, int nb) {
+  constexpr int W = Row<T>::W, R = 256 / L;
+  const int lane = threadIdx.x % L, rl = threadIdx.x / L;
+  for (long long r0 = (long long)blockIdx.x * R; r0 < rows; r0 += (long long)gridDim.x * R) {
+    const bool row = rl < rows - r0;
+    const T* xr = x + r0 * C;
+    signed char* q = to.q + r0 * C;
+    unsigned char* b = to.b + r0 * nb;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const Place at = place_in_row<W>(v * L + lane, C);
+      const bool live = row && at.live;
+      raw16 raw = {};
+      if (live) raw = Row<T>::template load<TAIL>(xr + (rl * C + at.col), at, C);
+      float f[W];
+      Row<T>::widen(raw, f);
+      own_only<TAIL>(at, f);
+      q8_keep<TAIL, L, W>(q + rl * C, b + rl * nb, at, live, f);
+    }
   }
 }
 
-template <typename T, int W>
-__global__ void __launch_bounds__(256) k_q8_unpack(Q8Ref from, T* __restrict__ out, long long chunks, int C, int nb) {
-  const int cpr = C / W;  // chunks of a row
-  const long long stride = (long long)gridDim.x * 256;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < chunks; i += stride) {
-    const long long r = i / cpr;
-    const int col = (int)(i - r * cpr) * W;
-    int q[W];
-    q8_load<W>(from.q, r * C + col, q);
-    const float s = q8_scale(from.b[r * nb + col / kQ8Block]);
-    float v[W];
+template <typename T, int L, int NV, bool TAIL>
+__global__ void __launch_bounds__(256) k_q8_unpack(Q8Ref from, T* __restrict__ out, long long rows, int C, int nb) {
+  constexpr int W = Row<T>::W, R = 256 / L;
+  const int lane = threadIdx.x % L, rl = threadIdx.x / L;
+  for (long long r0 = (long long)blockIdx.x * R; r0 < rows; r0 += (long long)gridDim.x * R) {
+    const signed char* q = from.q + r0 * C;
+    const unsigned char* b = from.b + r0 * nb;
+    T* o = out + r0 * C;
+    if (rl >= rows - r0) continue;
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = q8_value(q[j], s);
-    Chunk<T, W>::store(out, r * C + col, v);
+    for (int v = 0; v < NV; ++v) {
+      const Place at = place_in_row<W>(v * L + lane, C);
+      if (at.live) {
+        const auto w = q8_load<TAIL, W>(q + (rl * C + at.col), at, C);
+        float f[W];
+        q8_widen<W>(w, q8_step(b[rl * nb + at.block]), f);
+        Row<T>::template store<TAIL>(o + (rl * C + at.col), at, Row<T>::narrow(f));
+      }
+    }
   }
 }
 
 // out[i] = q[i] > 0 ? a[i] : 0 (out may be a)
-template <typename T, int W>
-__global__ void __launch_bounds__(256) k_relu_bwd_q8(const T* a, const signed char* __restrict__ q, T* out, long long chunks) {
-  const long long stride = (long long)gridDim.x * 256;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < chunks; i += stride) {
-    float v[W];
-    int y[W];
-    Chunk<T, W>::load(a, i * W, v);
-    q8_load<W>(q, i * W, y);
+template <typename T> __global__ void __launch_bounds__(256) k_relu_bwd_q8(const T* a, const signed char* __restrict__ q, T* out, long long n) {
+  constexpr int W = Row<T>::W;
+  for (long long i0 = (long long)blockIdx.x * (256 * W); i0 < n; i0 += (long long)gridDim.x * (256 * W)) {
+    const T* pa = a + i0;
+    const signed char* pq = q + i0;
+    T* po = out + i0;
+    const int i = threadIdx.x * W;
+    if (i + W <= n - i0) {
+      typename Row<T>::vec v = __builtin_bit_cast(typename Row<T>::vec, load_any<raw16>(pa + i));
+      const auto y = load_any<typename Bytes<W>::word>(pq + i);
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = y[j] > 0 ? v[j] : 0.f;
-    Chunk<T, W>::store(out, i * W, v);
+      for (int j = 0; j < W; ++j) v[j] = q8_at<W>(y, j) > 0 ? v[j] : (T)0.f;
+      store_any(po + i, __builtin_bit_cast(raw16, v));
+    } else {
+      for (int j = i; j < i + W && j < n - i0; ++j) po[j] = pq[j] > 0 ? pa[j] : (T)0.f;
+    }
   }
 }
 
 unsigned grid_for(long long items, int per_block) {
   return (unsigned)std::min<long long>((items + per_block - 1) / per_block, 1 << 20);
 }
-bool aligned(const void* p, size_t n) { return ((size_t)p & (n - 1)) == 0; }
 
-template <typename T> int launch_pack(const void* x, int64_t rows, int C, const Q8Ref& to, hipStream_t st) {
-  constexpr int W = 16 / sizeof(T);
-  const int nb = (C + kQ8Block - 1) / kQ8Block;
-  const long long blocks = (long long)rows * nb;
-  if (C % W == 0 && aligned(x, 16) && aligned(to.q, W))
-    hipLaunchKernelGGL((k_q8_pack<T, W>), dim3(grid_for(blocks, 256 / (kQ8Block / W))), dim3(256), 0, st, (const T*)x, to, blocks, C, nb);
-  else
-    hipLaunchKernelGGL((k_q8_pack<T, 1>), dim3(grid_for(blocks, 256 / kQ8Block)), dim3(256), 0, st, (const T*)x, to, blocks, C, nb);
-  SPC_LAUNCH_CHECK();
-  return SPCONV_OK;
-}
-template <typename T> int launch_unpack(const Q8Ref& from, int64_t rows, int C, void* out, hipStream_t st) {
-  constexpr int W = 16 / sizeof(T);
-  const int nb = (C + kQ8Block - 1) / kQ8Block;
-  if (C % W == 0 && aligned(out, 16) && aligned(from.q, W)) {
-    const long long chunks = (long long)rows * (C / W);
-    hipLaunchKernelGGL((k_q8_unpack<T, W>), dim3(grid_for(chunks, 256)), dim3(256), 0, st, from, (T*)out, chunks, C, nb);
-  } else {
-    const long long chunks = (long long)rows * C;
-    hipLaunchKernelGGL((k_q8_unpack<T, 1>), dim3(grid_for(chunks, 256)), dim3(256), 0, st, from, (T*)out, chunks, C, nb);
+// Widths that are whole blocks: every block is a row (no lane idles, whatever the width).
+void blocks_as_rows(long long* rows, int* C) {
+  if (*C % kQ8Block == 0) {
+    *rows *= *C / kQ8Block;
+    *C = kQ8Block;
   }
-  SPC_LAUNCH_CHECK();
-  return SPCONV_OK;
+}
+template <typename T> int launch_pack(const void* x, long long rows, int C, const Q8Ref& to, hipStream_t st) {
+  blocks_as_rows(&rows, &C);
+  return with_lanes<Row<T>::W>(C, [&](auto l) {
+    constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
+    hipLaunchKernelGGL((k_q8_pack<T, L, NV, decltype(l)::TAIL>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, (const T*)x, to, rows, C,
+                       (C + kQ8Block - 1) / kQ8Block);
+    SPC_LAUNCH_CHECK();
+    return (int)SPCONV_OK;
+  });
+}
+template <typename T> int launch_unpack(const Q8Ref& from, long long rows, int C, void* out, hipStream_t st) {
+  blocks_as_rows(&rows, &C);
+  return with_lanes<Row<T>::W>(C, [&](auto l) {
+    constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
+    hipLaunchKernelGGL((k_q8_unpack<T, L, NV, decltype(l)::TAIL>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, from, (T*)out, rows, C,
+                       (C + kQ8Block - 1) / kQ8Block);
+    SPC_LAUNCH_CHECK();
+    return (int)SPCONV_OK;
+  });
 }
 template <typename T> int launch_relu_bwd(const void* a, const signed char* q, int64_t n, void* out, hipStream_t st) {
-  constexpr int W = 16 / sizeof(T);
-  if (n % W == 0 && aligned(a, 16) && aligned(out, 16) && aligned(q, W))
-    hipLaunchKernelGGL((k_relu_bwd_q8<T, W>), dim3(grid_for(n / W, 256)), dim3(256), 0, st, (const T*)a, q, (T*)out, n / W);
-  else
-    hipLaunchKernelGGL((k_relu_bwd_q8<T, 1>), dim3(grid_for(n, 256)), dim3(256), 0, st, (const T*)a, q, (T*)out, n);
+  hipLaunchKernelGGL((k_relu_bwd_q8<T>), dim3(grid_for(n, 256 * Row<T>::W)), dim3(256), 0, st, (const T*)a, q, (T*)out, (long long)n);
   SPC_LAUNCH_CHECK();
   return SPCONV_OK;
 }

@@ -18,115 +18,228 @@ template <int O> __device__ __forceinline__ unsigned lane_across(unsigned v) {  
   else if constexpr (O == 8) return dpp<0x140>(v);  // row_mirror
   else return (unsigned)__shfl_xor((int)v, O);
 }
-template <int L, int O = 1> __device__ __forceinline__ float group_sum(float v) {
+template <int L, int O = 1> __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (O >= L) return v;
-  else return group_sum<L, O * 2>(v + __builtin_bit_cast(float, lane_across<O>(__builtin_bit_cast(unsigned, v))));
+  else return lanes_sum<L, O * 2>(v + __builtin_bit_cast(float, lane_across<O>(__builtin_bit_cast(unsigned, v))));
+}
+// The same for up to 256 lanes: beyond a wave through `part`, after a barrier that the whole workgroup reaches.  Two slots, used in
+// turn: whoever writes a slot again has passed the other one's barrier, which everyone reaches after reading this one.
+template <int L> __device__ __forceinline__ float group_sum(float v, float (*part)[4], int slot) {
+  if constexpr (L <= 64) {
+    return lanes_sum<L>(v);
+  } else {
+    v = lanes_sum<64>(v);
+    if (threadIdx.x % 64 == 0) part[slot][threadIdx.x / 64] = v;
+    __syncthreads();
+    const int first = threadIdx.x / L * (L / 64);
+    v = part[slot][first];
+#pragma unroll
+    for (int w = 1; w < L / 64; ++w) v += part[slot][first + w];
+    return v;
+  }
 }
 template <int L, int O = 1> __device__ __forceinline__ unsigned group_max(unsigned v) {
   if constexpr (O >= L) return v;
   else return group_max<L, O * 2>(max(v, lane_across<O>(v)));
 }
 
-// ---- W consecutive elements of a row, as fp32.  W elements of T make 16 bytes and stand at a multiple of them, or W is 1.
-template <typename T, int W> struct Chunk {
-  typedef T vec __attribute__((ext_vector_type(W), aligned(16)));
-  static __device__ __forceinline__ void load(const void* base, long long at, float (&v)[W]) {
-    const vec x = *reinterpret_cast<const vec*>(reinterpret_cast<const T*>(base) + at);
+// ---- vectors of a row: W consecutive elements that make 16 bytes, held as they are in memory.  Rows of odd widths start anywhere: the
+// hardware takes 16-byte accesses at any address, so one path serves every width.
+typedef unsigned int raw16 __attribute__((ext_vector_type(4)));
+typedef unsigned int raw8 __attribute__((ext_vector_type(2)));
+typedef float float4x __attribute__((ext_vector_type(4)));
+template <typename V> struct __attribute__((packed)) AnyAddress { V v; };
+template <typename V> __device__ __forceinline__ V load_any(const void* p) { return reinterpret_cast<const AnyAddress<V>*>(p)->v; }
+template <typename V> __device__ __forceinline__ void store_any(void* p, V v) { reinterpret_cast<AnyAddress<V>*>(p)->v = v; }
+
+// Where a lane's vector of a row of C channels stands.  The vector that ends a row whose width is no multiple of W reaches back over
+// its neighbour's channels (loaded with one access, like any other): its first `lo` elements are not its own and count as zero.
+// In rows of fewer than W channels `col` is negative and elements are taken one by one.
+struct Place {
+  int col;    // channel of element 0
+  int lo;     // own elements are [lo, W)
+  int block;  // of 32 channels, that the own elements lie in
+  bool live;  // there are any
+};
+template <int W> __device__ __forceinline__ Place place_in_row(int vector, int C) {
+  const int first = vector * W, n = C - first;
+  return {n >= W ? first : C - W, n >= W ? 0 : W - n, first / 32, n > 0};
+}
+
+template <typename T> struct Row {
+  static constexpr int W = 16 / sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(W)));
+
+  // p: element 0 of the vector.  TAIL: widths that are no multiple of W.
+  template <bool TAIL> static __device__ __forceinline__ raw16 load(const T* p, const Place& at, int C) {
+    if (!TAIL || C >= W) return load_any<raw16>(p);
+    vec x;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = p[max(i, at.lo)];
+    return __builtin_bit_cast(raw16, x);
+  }
+  template <bool TAIL> static __device__ __forceinline__ void store(T* p, const Place& at, raw16 r) {
+    if (!TAIL || at.lo == 0) {
+      store_any(p, r);
+      return;
+    }
+    const vec x = __builtin_bit_cast(vec, r);
+#pragma unroll
+    for (int i = 1; i < W; ++i)
+      if (i >= at.lo) p[i] = x[i];
+  }
+  static __device__ __forceinline__ void widen(raw16 r, float (&v)[W]) {
+    const vec x = __builtin_bit_cast(vec, r);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = (float)x[i];
   }
-  // rounds to nearest even; v then holds what was written
-  static __device__ __forceinline__ void store(void* base, long long at, float (&v)[W]) {
+  static __device__ __forceinline__ raw16 narrow(const float (&v)[W]) {  // to nearest even
     vec x;
 #pragma unroll
     for (int i = 0; i < W; ++i) x[i] = (T)v[i];
-    *reinterpret_cast<vec*>(reinterpret_cast<T*>(base) + at) = x;
+    return __builtin_bit_cast(raw16, x);
+  }
+};
+// what stands in front of a vector's own elements becomes zero
+template <bool TAIL, int W> __device__ __forceinline__ void own_only(const Place& at, float (&v)[W]) {
+  if constexpr (TAIL) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = (float)x[i];
+    for (int i = 0; i < W; ++i) v[i] = i >= at.lo ? v[i] : 0.f;
   }
-};
-template <typename T> struct Chunk<T, 1> {
-  static __device__ __forceinline__ void load(const void* base, long long at, float (&v)[1]) {
-    v[0] = (float)reinterpret_cast<const T*>(base)[at];
+}
+template <bool TAIL, int W> __device__ __forceinline__ void load_floats(const float* p, const Place& at, int C, float (&v)[W]) {
+  if (!TAIL || C >= W) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const float4x r = load_any<float4x>(p + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i + j] = r[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = p[max(i, at.lo)];
   }
-  static __device__ __forceinline__ void store(void* base, long long at, float (&v)[1]) {
-    const T x = (T)v[0];
-    reinterpret_cast<T*>(base)[at] = x;
-    v[0] = (float)x;
-  }
-};
+}
 
 // ---- 8-bit checkpoints.  A row is cut into blocks of 32 channels.  b: biased fp32 exponent of the block's largest magnitude, at
 // least 1, or 255 where the block has an infinity or a NaN; a channel is q * 2^(b - 133).
-// q has 8 bits and a sign, the step is a power of two: the value is exact in fp16, bf16 and fp32 alike (the step of an fp16
+// q has 7 bits and a sign, the step is a power of two: the value is exact in fp16, bf16 and fp32 alike (the step of an fp16
 // block is below fp16's smallest number only where every product is a multiple of that number), so a kernel that reads a
 // checkpoint sees what it would see in the unpacked tensor.
 constexpr int kQ8Block = 32;
-
-__device__ __forceinline__ unsigned q8_exponent(unsigned top) { return max(top >> 23, 1u); }  // top: bits of the largest |x|
-__device__ __forceinline__ int q8_quantise(float x, unsigned b) {
-  if (b >= 255u) return 0;
-  // v_ldexp: exact (2^(133 - b) itself can exceed fp32).  |x| < 2^(b - 126), so the product is below 128 and rounds to at
-  // most that; the clamp costs those 128 one step at most.
-  const float s = ldexpf(x, 133 - (int)b);
-  int q = (int)rintf(s);
-  q = min(max(q, -127), 127);
-  return q == 0 ? (x > 0.f) - (x < 0.f) : q;  // keeps the sign: a ReLU's gradient asks for it
-}
-// 2^(b - 127); infinite for b = 255, which turns q = 0 into a NaN
-__device__ __forceinline__ float q8_scale(unsigned b) { return __builtin_bit_cast(float, b << 23); }
-__device__ __forceinline__ float q8_value(int q, float scale) { return (float)q * 0.015625f * scale; }
-
-template <int W> struct Bytes;
-template <> struct Bytes<8> { typedef unsigned word __attribute__((ext_vector_type(2))); };
-template <> struct Bytes<4> { typedef unsigned word __attribute__((ext_vector_type(1))); };
-
-// W consecutive q of a row (a multiple of W bytes in, or W is 1)
-template <int W> __device__ __forceinline__ void q8_load(const signed char* base, long long at, int (&q)[W]) {
-  if constexpr (W == 1) {
-    q[0] = base[at];
-  } else {
-    const auto w = *reinterpret_cast<const typename Bytes<W>::word*>(base + at);
-#pragma unroll
-    for (int i = 0; i < W; ++i) q[i] = (int)(w[i / 4] << (24 - 8 * (i % 4))) >> 24;
-  }
-}
-template <int W> __device__ __forceinline__ void q8_store(signed char* base, long long at, const int (&q)[W]) {
-  if constexpr (W == 1) {
-    base[at] = (signed char)q[0];
-  } else {
-    typename Bytes<W>::word w;
-#pragma unroll
-    for (int j = 0; j < W / 4; ++j)
-      w[j] = (unsigned)(q[4 * j] & 255) | (unsigned)(q[4 * j + 1] & 255) << 8 | (unsigned)(q[4 * j + 2] & 255) << 16 |
-             (unsigned)q[4 * j + 3] << 24;
-    *reinterpret_cast<typename Bytes<W>::word*>(base + at) = w;
-  }
-}
 
 struct Q8Ref {  // a checkpoint: [rows][C] and [rows][ceil(C / 32)]
   signed char* q;
   unsigned char* b;
 };
 
-// A group of L lanes (32 / W of them, or all, make a block) writes W channels each of row r: v of columns col.., live: col < C.
-// Every lane of the wave takes part.
-template <int L, int W>
-__device__ __forceinline__ void q8_keep(const Q8Ref& to, long long r, int C, int nb, int col, bool live, const float (&v)[W]) {
-  constexpr int G = L < kQ8Block / W ? L : kQ8Block / W;
+// 2^(b - 133) (subnormal for the smallest b); infinite for b = 255, which turns q = 0 into a NaN
+__device__ __forceinline__ float q8_step(unsigned b) {
+  const float s = ldexpf(1.f, (int)b - 133);
+  return b == 255u ? __builtin_inff() : s;
+}
+template <int W> struct Bytes;  // the q of a vector
+template <> struct Bytes<8> { typedef raw8 word; };
+template <> struct Bytes<4> { typedef unsigned word __attribute__((ext_vector_type(1))); };
+
+template <bool TAIL, int W>
+__device__ __forceinline__ typename Bytes<W>::word q8_load(const signed char* p, const Place& at, int C) {
+  typedef typename Bytes<W>::word word;
+  if (!TAIL || C >= W) return load_any<word>(p);
+  word w = {};
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i / 4] |= (unsigned)(unsigned char)p[max(i, at.lo)] << (8 * (i % 4));
+  return w;
+}
+template <bool TAIL, int W> __device__ __forceinline__ void q8_store(signed char* p, const Place& at, typename Bytes<W>::word w) {
+  if (!TAIL || at.lo == 0) {
+    store_any(p, w);
+    return;
+  }
+#pragma unroll
+  for (int i = 1; i < W; ++i)
+    if (i >= at.lo) p[i] = (signed char)(w[i / 4] >> (8 * (i % 4)));
+}
+template <int W> __device__ __forceinline__ int q8_at(typename Bytes<W>::word w, int i) { return (signed char)(w[i / 4] >> (8 * (i % 4))); }
+template <int W> __device__ __forceinline__ void q8_widen(typename Bytes<W>::word w, float step, float (&v)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = (float)q8_at<W>(w, i) * step;
+}
+
+// The checkpoint of a vector, one of the G that make a block (aligned groups of G lanes; every lane of the group takes part, with zeros
+// where it has no elements).  What bounds a kernel that keeps two checkpoints is the vector unit as soon as an element takes more
+// than about 50 instructions; this takes 9.  Rounding is that of an addition: 1.5 * 2^23 + r has r to nearest even in its
+// low bits.
+template <int G, int W> __device__ __forceinline__ typename Bytes<W>::word q8_quantise(const float (&v)[W], unsigned& b) {
   unsigned top = 0;
-  if (live) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = max(top, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
-  }
-  const unsigned b = q8_exponent(group_max<G>(top));
-  if (live) {
-    int q[W];
+  for (int i = 0; i < W; ++i) top = max(top, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
+  top = group_max<G>(top);
+  b = max(top >> 23, 1u);
+  // 2^(133 - b) is a number from b = 6 on; below (magnitudes under 2^-121) v_ldexp scales.  Products are exact, except for values so
+  // far below the block's largest that they are kept for their sign alone.
+  const float inv = __builtin_bit_cast(float, (260u - max(b, 6u)) << 23);
+  float t[W];
 #pragma unroll
-    for (int i = 0; i < W; ++i) q[i] = q8_quantise(v[i], b);
-    q8_store<W>(to.q, r * C + col, q);
-    if (col % kQ8Block == 0) to.b[r * nb + col / kQ8Block] = (unsigned char)b;
+  for (int i = 0; i < W; ++i) t[i] = v[i] * inv;
+  if (__builtin_expect(__any(b < 6u && top != 0u), 0)) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) t[i] = b < 6u ? ldexpf(v[i], 133 - (int)b) : t[i];
   }
+  unsigned s[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    // (at most 127: 128 would be the rounding of values from 127.5 on; at least 1, by 0.75, where the value is not 0)
+    const float m = __builtin_amdgcn_fmed3f(__builtin_fabsf(t[i]), 0.75f, 127.f);
+    const float r = v[i] != 0.f ? __builtin_copysignf(m, v[i]) : 0.f;
+    s[i] = __builtin_bit_cast(unsigned, r + 12582912.f);
+  }
+  typename Bytes<W>::word w;
+#pragma unroll
+  for (int j = 0; j < W / 4; ++j) {
+    const unsigned lo = __builtin_amdgcn_perm(s[4 * j + 1], s[4 * j], 0x0C0C0400u), hi = __builtin_amdgcn_perm(s[4 * j + 3], s[4 * j + 2], 0x04000C0Cu);
+    w[j] = b < 255u ? lo | hi : 0u;
+  }
+  return w;
+}
+
+// A group of L lanes (32 / W of them, or all, make a block) writes a vector each of the row at q and b.
+template <bool TAIL, int L, int W>
+__device__ __forceinline__ void q8_keep(signed char* q, unsigned char* b, const Place& at, bool live, const float (&v)[W]) {
+  constexpr int G = L < kQ8Block / W ? L : kQ8Block / W;
+  unsigned e;
+  const auto w = q8_quantise<G, W>(v, e);
+  if (live) {
+    q8_store<TAIL, W>(q + at.col, at, w);
+    if (threadIdx.x % G == 0) b[at.block] = (unsigned char)e;
+  }
+}
+
+// Lanes of a row and vectors of a lane: as few lanes as hold the row with one vector each, up to a workgroup's 256, then more
+// vectors (all of a row's lanes in one wave, with 8 vectors or more each, did not fit the registers).  C is 1 to 4096.  Calls go with them as constants.
+template <int LANES, int VECTORS, bool TAIL_> struct Lanes {
+  static constexpr int L = LANES, NV = VECTORS;
+  static constexpr bool TAIL = TAIL_;
+};
+template <int W, typename F> int with_lanes(int C, F go) {
+  const int n = (C + W - 1) / W;
+  if (C % W == 0) {
+    if (n <= 4) return go(Lanes<4, 1, false>{});
+    if (n <= 8) return go(Lanes<8, 1, false>{});
+    if (n <= 16) return go(Lanes<16, 1, false>{});
+    if (n <= 32) return go(Lanes<32, 1, false>{});
+    if (n <= 64) return go(Lanes<64, 1, false>{});
+  }
+  if (n <= 4) return go(Lanes<4, 1, true>{});
+  if (n <= 8) return go(Lanes<8, 1, true>{});
+  if (n <= 16) return go(Lanes<16, 1, true>{});
+  if (n <= 32) return go(Lanes<32, 1, true>{});
+  if (n <= 64) return go(Lanes<64, 1, true>{});
+  if (n <= 128) return go(Lanes<128, 1, true>{});
+  if (n <= 256) return go(Lanes<256, 1, true>{});
+  if (n <= 512) return go(Lanes<256, 2, true>{});
+  if constexpr (W == 4) return go(Lanes<256, 4, true>{});
+  return SPCONV_EINVAL;
 }
 
 }  // namespace
