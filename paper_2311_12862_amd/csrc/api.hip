@@ -461,6 +461,13 @@ int run_igemm_op(spconv_op op, const void* src, const void* weights, spconv_kmap
   return run_kernel(km, *os.side, *plan, a, kc, st);
 }
 
+// Whether a weight gradient is taken from the map or over the pairs (wgrad_from_map); a call that names its pieces walks pairs.
+int wgrad_route(spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype, const spconv_config& c, hipStream_t st, bool* from_map) {
+  if (km->n_pairs < 0 && !km->pending) SPC_TRY(kmap_count_pairs(km, st, nullptr));
+  if (c.wgrad_pairs == 0 && km->wgrad_known_pairs == spconv_kmap::kNotAsked) km->wgrad_known_pairs = km->n_pairs;
+  *from_map = c.wgrad_pairs == 0 && wgrad_from_map(km, C_in, C_out, dtype);
+  return SPCONV_OK;
+}
 }  // namespace
 }  // namespace spc
 
@@ -730,13 +737,12 @@ SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km
     }
     return SPCONV_OK;
   }
-  if (km->n_pairs < 0 && !km->pending) SPC_TRY(kmap_count_pairs(km, st, nullptr));
-  if (c.wgrad_pairs == 0 && km->wgrad_known_pairs == spconv_kmap::kNotAsked) km->wgrad_known_pairs = km->n_pairs;
-  if (c.wgrad_pairs == 0 && wgrad_from_map(km, C_in, C_out, dtype))
-    return wgrad_map_run(km, feats, dout, C_in, C_out, dtype, dweights, st);
+  bool from_map;
+  SPC_TRY(wgrad_route(km, C_in, C_out, dtype, c, st, &from_map));
+  if (from_map) return wgrad_map_run(km, feats, dout, C_in, C_out, dtype, dweights, st);
   PairList* pl = nullptr;
   SPC_TRY(pair_list_get(km, st, &pl));
-  return wgrad_run(km, *pl, c.wgrad_pairs, feats, dout, C_in, C_out, dtype, dweights, st);
+  return wgrad_run(km, *pl, c.wgrad_pairs, feats, nullptr, dout, C_in, C_out, dtype, dweights, st);
 }
 
 SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
@@ -748,6 +754,16 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
   hipStream_t st = (hipStream_t)stream;
   spconv_config c;
   SPC_TRY(resolve_config(cfg, dtype, &c));
+  if (wgrad_takes_q8(km, kept, C_in, dtype)) {
+    km->last_stream = st;
+    bool from_map;
+    SPC_TRY(wgrad_route(km, C_in, C_out, dtype, c, st, &from_map));
+    if (!from_map) {
+      PairList* pl = nullptr;
+      SPC_TRY(pair_list_get(km, st, &pl));
+      return wgrad_run(km, *pl, c.wgrad_pairs, nullptr, kept, dout, C_in, C_out, dtype, dweights, st);
+    }
+  }
   SPC_TRY(km->unpacked.reserve((size_t)km->n_in * C_in * (dtype == SPCONV_F32 ? 4 : 2)));
   if (km->n_in > 0) SPC_TRY(q8_unpack(kept, km->n_in, C_in, dtype, km->unpacked.p, st));
   return spconv_wgrad(km->unpacked.p, dout, km, C_in, C_out, dtype, cfg, dweights, stream);

@@ -24,7 +24,7 @@
 // last-level cache at about 7 TB/s); 96 -> 96: 218 -> 191 us (192-byte rows touch two lines); 32 -> 32: 98 -> 86 us (64-byte
 // rows: 5 TB/s at best).  680k pairs f16, 64 -> 128: 57 -> 48 us.  128k pairs fp32, 64 -> 64: 112 -> 26 us.
 #include "common.h"
-#include "lds_tiles.h"
+#include "wgrad.h"
 
 #include <algorithm>
 #include <atomic>
@@ -34,62 +34,6 @@
 
 namespace spc {
 namespace {
-
-struct Split {
-  int pieces;    // at most so many (grid, partial tiles)
-  int length;    // pairs of a piece as asked for, or 0: chosen by
-  float weight;  // sqrt(time of a pair in a piece / time of a partial tile), and at least
-  int unit;      // so many
-  int per_round;  // pieces that make one workgroup per CU
-};
-
-struct WgradParams {
-  const void* feats;   // [n_in][C_in]
-  const void* dout;    // [n_out][C_out]
-  const int2* pairs;   // (n, j), offset-major
-  const int* seg;      // [V+1]
-  float* partial;      // [piece][C_in][C_out]
-  unsigned feats_bytes, dout_bytes, pairs_bytes;
-  int C_in, C_out, V;
-  Split split;
-};
-
-constexpr unsigned kNoRow = 0xFFFFC000u;  // beyond every buffer
-
-// Pairs per piece; computed by every workgroup, as the pair count may only be known on the device.
-// g pieces take time ~ pairs / g (a workgroup's serial part) + g * (a tile written and read): least at g ~ sqrt(pairs).
-// Long pieces then go down to whole rounds of one workgroup per CU, each offset's last piece counted: two workgroups of a CU
-// gather at half the rate each, and the launch waits for the CUs that have one more (421k pairs 128 -> 128, 410 pieces 47.2 us,
-// 249 pieces 40.9; 256 -> 128, 604 workgroups 80.0, 510 69.1).  Not where that takes too many of them (271k pairs 256 ->
-// 128, 496 workgroups 47.9 us, 256 57.1), nor where pieces are short, so that their start is what counts (127k pairs 256
-// -> 128: 32.9 us, in one round 35.3).
-__device__ __forceinline__ int split_length(const Split& s, int pairs, int V) {
-  if (s.length > 0) return s.length;
-  int g = min(s.pieces - V, (int)(s.weight * sqrtf((float)pairs)) + 1);
-  const int whole = (g + V) / s.per_round * s.per_round - V;
-  const int least = s.per_round == 256 ? g / 2 : g - g / 4;  // (a single column of tiles: rounds are finer)
-  if (whole >= least && pairs / g >= 900) g = whole;
-  return max(s.unit, (pairs + g - 1) / g);
-}
-// Lane k < V of a wave: the pieces of the offsets before k, and of k.
-struct Pieces {
-  int before, count;
-};
-__device__ __forceinline__ Pieces pieces_of(const Split& s, int bound, int V, int lane) {  // bound: lane k <= V holds seg[k]
-  const int length = split_length(s, __builtin_amdgcn_readlane(bound, V), V);
-  const int pairs = __shfl_down(bound, 1) - bound;
-  const int count = lane < V ? (pairs + length - 1) / length : 0;
-  int incl = count;
-  for (int o = 1; o < 32; o <<= 1) {
-    const int up = __shfl_up(incl, o);
-    if (lane >= o) incl += up;
-  }
-  return {incl - count, count};
-}
-
-template <int N> __device__ __forceinline__ void wait_loads() {  // all but the N youngest; own LDS reads are done as well
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(N) : "memory");
-}
 
 // TI x TO (channels of x, of dy) per workgroup; NWI x NWO waves share a batch, or (NWK > 1) each wave has its own.
 // S stages.
@@ -111,34 +55,6 @@ template <typename T, int TI, int TO, int NWI, int NWO, int NWK, int S> struct W
   static_assert((LX + LD) % NW == 0 && x_bytes % 1024 == 0 && d_bytes % 1024 == 0, "whole loads");
   static_assert(L * (S - 2) + S - 2 < 64, "vmcnt");
 };
-
-// Where chunk c (16 bytes) of row r of a staged batch stands.  16-bit types: the transposing read of 32 lanes takes rows
-// r..r+3 and r+8..r+11 at one 32-byte block each; fp32: four rows at one 64-byte block.  Eight (four) blocks span
-// the LDS banks, so the block number is XORed (six blocks: rotated) by the row.
-template <int E, int CPR> __device__ __forceinline__ int chunk_block_shift(int r) {
-  if constexpr (E == 4) return CPR >= 16 ? (r & 3) : (r >> 1) & 1;
-  else if constexpr (CPR == 4) return (r >> 3) & 1;
-  else if constexpr (CPR == 8) return ((r >> 1) & 1) | (((r >> 3) & 1) << 1);
-  else if constexpr (CPR == 12) return (r >> 3) & 1;
-  else return (r & 3) | (((r >> 3) & 1) << 2);
-}
-// block b of row r stands at block place_of(b), and place q holds block block_at(q)
-template <int E, int CPR> __device__ __forceinline__ int place_of(int b, int r) {
-  if constexpr (E == 2 && CPR == 12) {
-    const int q = b + chunk_block_shift<E, CPR>(r);
-    return q >= 6 ? q - 6 : q;
-  } else {
-    return b ^ chunk_block_shift<E, CPR>(r);
-  }
-}
-template <int E, int CPR> __device__ __forceinline__ int block_at(int q, int r) {
-  if constexpr (E == 2 && CPR == 12) {
-    const int b = q - chunk_block_shift<E, CPR>(r);
-    return b < 0 ? b + 6 : b;
-  } else {
-    return q ^ chunk_block_shift<E, CPR>(r);
-  }
-}
 
 template <typename T, int TI, int TO, int NWI, int NWO, int NWK, int S>
 __global__ void __launch_bounds__(NWI* NWO* NWK * 64) k_wgrad(const WgradParams p) {
@@ -822,13 +738,20 @@ int64_t wgrad_auto_pairs(const spconv_kmap* km, int C_in, int C_out, spconv_dtyp
   return std::max<int64_t>(s.unit, ceil_div(pairs, s.pieces - km->V));
 }
 
-// piece_pairs: pairs of a piece, 0: chosen here.
-int wgrad_run(spconv_kmap* km, const PairList& pl, int64_t piece_pairs, const void* feats, const void* dout, int C_in, int C_out,
-              spconv_dtype dtype, float* dweights, hipStream_t st) {
+// Whether a checkpoint is gathered as it is (wgrad_q8.hip, with both sides measured: it is ahead of unpacking on all but a few
+// shapes, and there within 6 %); else it is unpacked first: fp32 layers, whose gradient the matrix instructions bound, rows that are no
+// whole 16-byte pieces, and the planes of a K = 5 map, which would each convert their pairs.
+bool wgrad_takes_q8(const spconv_kmap* km, const spconv_q8* kept, int C_in, spconv_dtype dtype) {
+  return dtype != SPCONV_F32 && C_in % 16 == 0 && ((size_t)kept->data & 15) == 0 && km->groups.empty();
+}
+
+// piece_pairs: pairs of a piece, 0: chosen here.  kept: in the place of feats
+int wgrad_run(spconv_kmap* km, const PairList& pl, int64_t piece_pairs, const void* feats, const spconv_q8* kept, const void* dout,
+              int C_in, int C_out, spconv_dtype dtype, float* dweights, hipStream_t st) {
   const int V = km->V;
   const int elems = C_in * C_out;
   const size_t e = dtype == SPCONV_F32 ? 4 : 2;
-  const uint64_t feats_bytes = (uint64_t)km->n_in * C_in * e, dout_bytes = (uint64_t)km->n_out * C_out * e;
+  const uint64_t feats_bytes = (uint64_t)km->n_in * C_in * (kept ? 1 : e), dout_bytes = (uint64_t)km->n_out * C_out * e;
   const uint64_t pairs_bytes = (uint64_t)round_up(std::max<int64_t>(pl.cap, 0), 2) * 8;
   const bool fits = feats_bytes < kNoRow && dout_bytes < kNoRow && pairs_bytes < kNoRow;  // buffer descriptors address 32 bits
   if (dtype != SPCONV_F32 && !fits) return SPCONV_EINVAL;
@@ -843,7 +766,11 @@ int wgrad_run(spconv_kmap* km, const PairList& pl, int64_t piece_pairs, const vo
     p.split = split_for(t, ceil_div(C_in, tile) * ceil_div(C_out, tile), V, pl.cap);
   }
   SPC_TRY(km->scratch.reserve((size_t)p.split.pieces * elems * sizeof(float)));
-  p.feats = feats;
+  p.feats = kept ? kept->data : feats;
+  if (kept) {
+    p.exps = kept->exps;
+    p.exps_bytes = (unsigned)((uint64_t)km->n_in * ceil_div(C_in, 32));
+  }
   p.dout = dout;
   p.pairs = pl.pairs.as<int2>();
   p.seg = pl.seg.as<int>();
@@ -856,7 +783,9 @@ int wgrad_run(spconv_kmap* km, const PairList& pl, int64_t piece_pairs, const vo
   p.V = V;
   if (pl.cap > 0) {
     const dim3 grid((unsigned)p.split.pieces, (unsigned)ceil_div(C_in, tile), (unsigned)ceil_div(C_out, tile));
-    if (dtype == SPCONV_F32 && !fits) {
+    if (kept) {
+      SPC_TRY(wgrad_q8_launch(p, tile, dtype, grid, st));
+    } else if (dtype == SPCONV_F32 && !fits) {
       hipLaunchKernelGGL(k_wgrad_f32, grid, dim3(256), 0, st, p);
       SPC_LAUNCH_CHECK();
     } else {

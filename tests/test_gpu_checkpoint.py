@@ -203,3 +203,39 @@ def test_offsets_beyond_32_bits():
     out = sp.q8_unpack(kept, torch.bfloat16, x)
     assert torch.equal(out[-3000:].double(), unpack64(q, b))
     assert torch.equal(sp.ew(sp.EW_RELU_BWD, out, kept)[-3000:], out[-3000:].relu())
+
+
+@pytest.mark.parametrize("ci,co", [(16, 16), (32, 32), (48, 64), (64, 64), (96, 96), (80, 40), (112, 128), (256, 256), (400, 72)])
+@pytest.mark.parametrize("dtype", DTS)
+@pytest.mark.parametrize("kind", ["sub3", "down", "dense"])
+def test_wgrad_has_the_bits_of_the_unpacked_tensor(ci, co, dtype, kind):
+    """The values are exact in every type and the sums' order is the tensor's."""
+    import paper_2311_12862_amd as sp
+    km = _map(kind)
+    x = _values(km.n_in, ci, dtype, 9)
+    x[3] = 0
+    kept, d = sp.q8_pack(x), _values(km.n_out, co, dtype, 10)
+    for pieces in (0, 1, 33, 4000) if kind == "sub3" else (0,):
+        cfg = sp.Config(wgrad_pairs=pieces) if pieces else None
+        assert torch.equal(sp.wgrad(kept, d, km, cfg), sp.wgrad(sp.q8_unpack(kept, dtype), d, km, cfg)), pieces
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_wgrad_of_every_exponent(dtype):
+    """Blocks of every size that the type has, subnormal ones among them, and a checkpoint whose data stands at an odd address."""
+    import paper_2311_12862_amd as sp
+    km = _map("one", 700)
+    low, high = (-24, 15) if dtype == torch.float16 else (-133, 127)
+    x = torch.randn(km.n_in, 64, device="cuda", dtype=torch.float64).clamp(-1, 1)
+    x = (x * torch.tensor([2.0 ** (low + i % (high - low + 1)) for i in range(km.n_in)], device="cuda", dtype=torch.float64)[:, None]).to(dtype)
+    d = torch.zeros(km.n_out, 64, dtype=dtype, device="cuda")
+    kept = sp.q8_pack(x)
+    room = torch.zeros(km.n_in * 64 + 1, dtype=torch.int8, device="cuda")
+    room[1:] = kept.data.flatten()
+    odd = sp.Checkpoint(room[1:].view(km.n_in, 64), kept.exps)
+    for row in range(0, km.n_in, 41):       # one row at a time: every value of it comes out as it is
+        d.zero_()
+        d[row, 5] = 1
+        want = unpack64(kept.data[row:row + 1], kept.exps[row:row + 1])[0]
+        for c in (kept, odd):
+            assert torch.equal(sp.wgrad(c, d, km)[0, :, 5].double(), want), row
