@@ -395,21 +395,21 @@ def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=N
 
 
 def _wgrad_q8(kept, dout, kmap, cfg, out, stream):
-    dt = _row_args(dout)
-    if dout.shape[0] != kmap.n_out or kept.rows != kmap.n_in:
-        raise SpconvError(-5, f"rows of the checkpoint ({kept.rows}) or of dout {tuple(dout.shape)} do not fit the kmap "
+    dt, shape, dev = _row_args(dout)
+    if shape[0] != kmap.n_out or kept.rows != kmap.n_in:
+        raise SpconvError(-5, f"rows of the checkpoint ({kept.rows}) or of dout {tuple(shape)} do not fit the kmap "
                               f"({kmap.n_in} in, {kmap.n_out} out)")
-    if kept.get_device() != dout.get_device():
+    if kept.get_device() != dev:
         raise ValueError(f"tensors on {dout.device} and {kept.device}")
-    if dout.get_device() != _device_now():
-        with torch.cuda.device(dout.device):
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return _wgrad_q8(kept, dout, kmap, cfg, out, stream)
-    c_in, c_out = kept.channels, dout.shape[1]
+    c_in, c_out = kept.channels, shape[1]
     if out is None:
         out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
     else:
         _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
-    status = _LIB.spconv_wgrad_q8(C.byref(kept.ref), _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
+    status = _LIB.spconv_wgrad_q8(kept.byref, _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
                                   _stream(stream))
     if status:
         _check(status, "spconv_wgrad_q8")
@@ -480,19 +480,17 @@ def ew(op: int, a, b=None, out=None, stream=None):
 def _relu_bwd_q8(op, a, kept, out, stream):
     if op != EW_RELU_BWD:
         raise ValueError("a Checkpoint stands for the output of EW_RELU_BWD only")
-    dt = _row_args(a)
-    if a.shape != (kept.rows, kept.channels):
+    dt, shape, dev = _row_args(a)
+    if shape != (kept.rows, kept.channels):
         raise ValueError("shape mismatch")
-    if kept.get_device() != a.get_device():
-        raise ValueError(f"tensors on {a.device} and {kept.device}")
-    if a.get_device() != _device_now():
-        with torch.cuda.device(a.device):
+    ref = _kept_like(kept, a, shape, dev)
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return _relu_bwd_q8(op, a, kept, out, stream)
     if out is None:
         out = torch.empty_like(a)
-    else:
-        _out_tensor(out, a.shape, a.dtype, a)
-    status = (_LIB or load_library()).spconv_relu_bwd_q8(_ptr(a), C.byref(kept.ref), _ptr(out), a.numel(), dt, _stream(stream))
+    status = (_LIB or load_library()).spconv_relu_bwd_q8(_ptr(a), ref, _like(out, a, shape, dev), kept.rows * kept.channels, dt,
+                                                         _stream(stream))
     if status:
         _check(status, "spconv_relu_bwd_q8")
     return out
@@ -522,46 +520,47 @@ def _device_now():
 
 
 def _row_args(x):
-    """The data type's number of a tensor [rows, channels]; what is none raises."""
-    dt = _DTYPES.get(x.dtype)
-    if dt is None or x.ndim != 2 or not x.is_cuda or not x.is_contiguous():
+    """Data type's number, shape and device of a tensor [rows, channels]; what is none raises."""
+    dt, shape, dev = _DTYPES.get(x.dtype), x.shape, x.get_device()
+    if dt is None or len(shape) != 2 or dev < 0 or not x.is_contiguous():
         _dev_tensor(x)
-        raise ValueError(f"expected a tensor [rows, channels] of {', '.join(map(str, _DTYPES))}, got {tuple(x.shape)} of {x.dtype}")
-    return dt
+        raise ValueError(f"expected a tensor [rows, channels] of {', '.join(map(str, _DTYPES))}, got {tuple(shape)} of {x.dtype}")
+    return dt, shape, dev
 
 
-def _like(t, x):
-    """t: a tensor that a call takes or fills beside x, of the same shape, type and device."""
-    if t.dtype is not x.dtype or t.shape != x.shape or not t.is_contiguous() or t.get_device() != x.get_device():
-        _out_tensor(t, x.shape, x.dtype, x)
-    return t
+def _like(t, x, shape, dev):
+    """Address of a tensor that a call takes or fills beside x, of the same shape, type and device."""
+    if t.dtype is not x.dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _out_tensor(t, shape, x.dtype, x)
+    return t.data_ptr() or None
 
 
-def _kept_like(kept, x):
+def _kept_like(kept, x, shape, dev):
+    """The checkpoint of a tensor like x, for the C call."""
     if not isinstance(kept, Checkpoint):
         raise ValueError(f"expected a Checkpoint, got {type(kept).__name__}")
-    if x.shape != (kept.rows, kept.channels):
-        raise SpconvError(-5, f"the checkpoint is {(kept.rows, kept.channels)}, the tensor {tuple(x.shape)}")
-    if kept.get_device() != x.get_device():
+    if (kept.rows, kept.channels) != shape:
+        raise SpconvError(-5, f"the checkpoint is {(kept.rows, kept.channels)}, the tensor {tuple(shape)}")
+    if kept.get_device() != dev:
         raise ValueError(f"tensors on {x.device} and {kept.device}")
-    return C.byref(kept.ref)
+    return kept.byref
 
 
-def _floats(t, shape, x):
+def _floats(t, shape, x, dev):
     """Address of fp32 values that a call reads beside x."""
-    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != x.get_device():
+    if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         _dev_tensor(t, torch.float32)
         if t.shape != shape:
             raise SpconvError(-5, f"expected fp32 values {shape}, got {tuple(t.shape)}")
         raise ValueError(f"tensors on {x.device} and {t.device}")
-    return t.data_ptr()
+    return t.data_ptr() or None
 
 
 class Checkpoint:
     """An activation [rows, channels] kept in 8 bits (spconv_q8): data int8 [rows, channels], exps uint8
     [rows, ceil(channels / 32)].  What a backward pass reads an activation for takes a Checkpoint in its place: `wgrad`,
     `layer_norm_bwd` and the gradient through a ReLU, `ew(EW_RELU_BWD, ...)`."""
-    __slots__ = ("rows", "channels", "ref", "_data", "_exps")
+    __slots__ = ("rows", "channels", "byref", "_data", "_exps")   # byref: the spconv_q8 of it, for the C calls
 
     def __init__(self, data, exps):
         _dev_tensor(data, torch.int8)
@@ -572,7 +571,7 @@ class Checkpoint:
             raise ValueError(f"tensors on {data.device} and {exps.device}")
         self.rows, self.channels = data.shape
         self._data, self._exps = data, exps
-        self.ref = Q8(_ptr(data), _ptr(exps))
+        self.byref = C.byref(Q8(_ptr(data), _ptr(exps)))
 
     @classmethod
     def empty(cls, rows: int, channels: int, device=_CUDA) -> "Checkpoint":
@@ -587,7 +586,7 @@ class Checkpoint:
         base = self._data.data_ptr()
         if base == 0 and rows:
             raise ValueError("expected a contiguous device tensor")
-        self.ref = Q8(base or None, base + at or None)
+        self.byref = C.byref(Q8(base or None, base + at or None))
         return self
 
     def _views(self):
@@ -616,14 +615,15 @@ class Checkpoint:
 
 def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """spconv_q8_pack: the 8-bit checkpoint of x [rows, channels]."""
-    dt = _row_args(x)
-    if x.get_device() != _device_now():
-        with torch.cuda.device(x.device):
+    dt, shape, dev = _row_args(x)
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return q8_pack(x, out, stream)
-    rows, channels = x.shape
+    rows, channels = shape
     if out is None:
-        out = Checkpoint.empty(rows, channels, x.device)
-    status = (_LIB or load_library()).spconv_q8_pack(_ptr(x), rows, channels, dt, _kept_like(out, x), _stream(stream))
+        out = Checkpoint.empty(rows, channels)
+    status = (_LIB or load_library()).spconv_q8_pack(_ptr(x), rows, channels, dt, _kept_like(out, x, shape, dev),
+                                                     _stream(stream))
     if status:
         _check(status, "spconv_q8_pack")
     return out
@@ -634,15 +634,16 @@ def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
     dt = _DTYPES.get(dtype)
     if dt is None:
         raise ValueError(f"unsupported dtype {dtype}")
-    if kept.get_device() != _device_now():
-        with torch.cuda.device(kept.device):
+    dev = kept.get_device()
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return q8_unpack(kept, dtype, out, stream)
-    shape = (kept.rows, kept.channels)
+    rows, channels = kept.rows, kept.channels
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=kept.device)
+        out = kept._data.new_empty((rows, channels), dtype=dtype)
     else:
-        _out_tensor(out, shape, dtype, kept)
-    status = (_LIB or load_library()).spconv_q8_unpack(C.byref(kept.ref), *shape, dt, _ptr(out), _stream(stream))
+        _out_tensor(out, (rows, channels), dtype, kept)
+    status = (_LIB or load_library()).spconv_q8_unpack(kept.byref, rows, channels, dt, _ptr(out), _stream(stream))
     if status:
         _check(status, "spconv_q8_unpack")
     return out
@@ -653,65 +654,71 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     """spconv_layer_norm_fwd: (y, stats) with y = act(norm(x) * weight + bias + residual), x and y [rows, channels],
     weight and bias fp32 [channels], stats fp32 [rows, 2] = (mean, 1 / std) for layer_norm_bwd.  keep_x and keep_y are
     filled with checkpoints of x and y in the same pass."""
-    dt = _row_args(x)
-    if x.get_device() != _device_now():
-        with torch.cuda.device(x.device):
+    dt, shape, dev = _row_args(x)
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return layer_norm_fwd(x, weight, bias, eps, relu, residual, out, keep_x, keep_y, stream)
-    rows, channels = x.shape
-    w = None if weight is None else _floats(weight, (channels,), x)
-    b = None if bias is None else _floats(bias, (channels,), x)
-    if residual is not None:
-        _like(residual, x)
-    kept_x = None if keep_x is None else _kept_like(keep_x, x)
-    kept_y = None if keep_y is None else _kept_like(keep_y, x)
-    out = torch.empty_like(x) if out is None else _like(out, x)
+    rows, channels = shape
+    w = None if weight is None else _floats(weight, (channels,), x, dev)
+    b = None if bias is None else _floats(bias, (channels,), x, dev)
+    res = None if residual is None else _like(residual, x, shape, dev)
+    kept_x = None if keep_x is None else _kept_like(keep_x, x, shape, dev)
+    kept_y = None if keep_y is None else _kept_like(keep_y, x, shape, dev)
+    if out is None:
+        out = torch.empty_like(x)
+    y = _like(out, x, shape, dev)
     stats = x.new_empty((rows, 2), dtype=torch.float32)
     status = (_LIB or load_library()).spconv_layer_norm_fwd(
-        _ptr(x), None if residual is None else _ptr(residual), w, b, eps, 1 if relu else 0, rows, channels, dt, _ptr(out),
-        _ptr(stats), kept_x, kept_y, _stream(stream))
+        _ptr(x), res, w, b, eps, 1 if relu else 0, rows, channels, dt, y, _ptr(stats), kept_x, kept_y, _stream(stream))
     if status:
         _check(status, "spconv_layer_norm_fwd")
     return out, stats
+
+
+_bwd_workspace = {}   # channels: bytes
 
 
 def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = False, affine: bool = True, stream=None):
     """spconv_layer_norm_bwd: (dx, dweight, dbias, dresidual) for a layer_norm_fwd that left stats.  x: its input or the
     Checkpoint of it; gate: its output or the Checkpoint of it where it had a ReLU.  dweight and dbias are fp32 [channels]
     (None for affine=False), dresidual is None unless residual is set."""
-    dt = _row_args(dout)
-    if dout.get_device() != _device_now():
-        with torch.cuda.device(dout.device):
+    dt, shape, dev = _row_args(dout)
+    if dev != _device_now():
+        with torch.cuda.device(dev):
             return layer_norm_bwd(dout, x, stats, weight, gate, residual, affine, stream)
-    rows, channels = dout.shape
-    st_ptr = _floats(stats, (rows, 2), dout)
-    w = None if weight is None else _floats(weight, (channels,), dout)
+    rows, channels = shape
+    stats_ptr = _floats(stats, (rows, 2), dout, dev)
+    w = None if weight is None else _floats(weight, (channels,), dout, dev)
     x_ptr = kept_x = y_ptr = kept_y = None
     if x is None:
         raise ValueError("x is the norm's input or its Checkpoint")
     if isinstance(x, Checkpoint):
-        kept_x = _kept_like(x, dout)
+        kept_x = _kept_like(x, dout, shape, dev)
     else:
-        x_ptr = _ptr(_like(x, dout))
+        x_ptr = _like(x, dout, shape, dev)
     if isinstance(gate, Checkpoint):
-        kept_y = _kept_like(gate, dout)
+        kept_y = _kept_like(gate, dout, shape, dev)
     elif gate is not None:
-        y_ptr = _ptr(_like(gate, dout))
+        y_ptr = _like(gate, dout, shape, dev)
     lib = _LIB or load_library()
     dx = torch.empty_like(dout)
     dres = torch.empty_like(dout) if residual else None
     dweight = dbias = dw_ptr = db_ptr = workspace = ws_ptr = None
     need = 0
     if affine:
-        need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
-        if need < 0:
-            _check(need, "spconv_layer_norm_bwd_workspace")
-        dweight = dout.new_empty((channels,), dtype=torch.float32)
-        dbias = dout.new_empty((channels,), dtype=torch.float32)
-        workspace = dout.new_empty((need,), dtype=torch.int8)
+        need = _bwd_workspace.get(channels)
+        if need is None:
+            need = lib.spconv_layer_norm_bwd_workspace(0, channels)
+            if need < 0:
+                _check(need, "spconv_layer_norm_bwd_workspace")
+            _bwd_workspace[channels] = need
+        dweight = stats.new_empty((channels,))
+        dbias = stats.new_empty((channels,))
+        workspace = stats.new_empty((need // 4,))
         dw_ptr, db_ptr, ws_ptr = dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr()
     st = _stream(stream)
-    status = lib.spconv_layer_norm_bwd(_ptr(dout), x_ptr, kept_x, y_ptr, kept_y, w, st_ptr if rows else None, rows, channels, dt,
-                                       _ptr(dx), None if dres is None else _ptr(dres), dw_ptr, db_ptr, ws_ptr, need, st)
+    status = lib.spconv_layer_norm_bwd(_ptr(dout), x_ptr, kept_x, y_ptr, kept_y, w, stats_ptr, rows, channels, dt, _ptr(dx),
+                                       None if dres is None else _ptr(dres), dw_ptr, db_ptr, ws_ptr, need, st)
     if status:
         _check(status, "spconv_layer_norm_bwd")
     if workspace is not None and stream is not None and st != _stream(None):
