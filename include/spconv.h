@@ -334,8 +334,8 @@ SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km
  * to 0.  So a value is off by at most half a step - one step where it is kept from rounding to 128 or to 0 - which is
  * 2^-7 (2^-6) of the block's largest magnitude; its sign is always right.  A block with an infinity or a NaN has b = 255 and
  * q = 0, and stands for NaN throughout.
- * C is 1 to 4096, rows * C at most 2^40.  Both pointers belong to the caller; no alignment is needed (16-byte aligned rows of
- * tensors and 8-byte aligned rows of data are the fast case). */
+ * Both pointers belong to the caller and need no alignment; C is 1 to 4096, rows * C at most 2^40.  Rows with a large offset
+ * (|mean| far above the spread) lose their spread to it: the step goes by the largest magnitude. */
 typedef struct spconv_q8 {
   int8_t* data;
   uint8_t* exps;
@@ -353,7 +353,8 @@ SPCONV_API int spconv_q8_unpack(const spconv_q8* kept, int64_t rows, int C, spco
 SPCONV_API int spconv_relu_bwd_q8(const void* dout, const spconv_q8* kept, void* out, int64_t n, spconv_dtype dtype, void* stream);
 
 /* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout.  The values are exact in dtype: the result is
- * that of spconv_wgrad on the unpacked tensor. */
+ * that of spconv_wgrad on the unpacked tensor.  16-bit layers of C_in % 16 == 0 on kmaps of K < 5 gather data itself where it is 16-byte
+ * aligned; others unpack it first, into memory that the kmap then keeps (one call before a capture makes it). */
 SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
                                const spconv_config* cfg_or_null, float* dweights, void* stream);
 
@@ -366,7 +367,7 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
  *   stats            device fp32 [rows][2] receives (m, r) of each row for the backward pass; may be NULL
  *   keep_x, keep_y   receive checkpoints of x and of y (as written) in the same pass: what spconv_q8_pack makes of them;
  *                    each may be NULL
- * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
+ * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  mean + eps counts as 2^-126 where it is less.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
  * `stream` and allocates nothing.  EINVAL: null pointers, sizes, dtype, relu, eps negative or NaN. */
 SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual_or_null, const float* weight_or_null,
                                      const float* bias_or_null, float eps, int relu, int64_t rows, int C, spconv_dtype dtype,

@@ -161,7 +161,12 @@ struct spconv_kmap {
   // the parts of a split.  Offset k of the whole map is offset k % 25 of plane k / 25.
   std::vector<std::unique_ptr<spconv_kmap>> groups;
   spc::DevBuf scratch;    // split partial sums / wgrad partial tiles
-  spc::DevBuf unpacked;   // the tensor of a checkpoint that wgrad reads
+  // The tensor of a checkpoint that wgrad reads.  Smaller ones that it took the place of stay: a captured graph may replay on them.
+  struct Unpacked {
+    spc::DevBuf buf;
+    std::unique_ptr<Unpacked> smaller;
+  };
+  std::unique_ptr<Unpacked> unpacked;
   // build whose status was not read yet: the pinned block the probe kernel publishes flags and
   // pair count to, with the event that marks the probe's completion
   void* pending_host = nullptr;

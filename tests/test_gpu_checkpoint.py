@@ -239,3 +239,26 @@ def test_wgrad_of_every_exponent(dtype):
         want = unpack64(kept.data[row:row + 1], kept.exps[row:row + 1])[0]
         for c in (kept, odd):
             assert torch.equal(sp.wgrad(c, d, km)[0, :, 5].double(), want), row
+
+
+def test_wgrad_captured_then_a_larger_layer():
+    """A captured call that unpacks replays on its own room after a wider layer of the kmap took a larger one."""
+    import paper_2311_12862_amd as sp
+    km, other = _map("sub3"), _map("sub3", 1500)
+    x, d = _values(km.n_in, 24, torch.float16, 1), _values(km.n_out, 16, torch.float16, 2)
+    kept = sp.q8_pack(x)
+    sp.wgrad(kept, d, km)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = sp.wgrad(kept, d, km)
+    for replay in range(3):
+        sp.q8_pack(_values(km.n_in, 24, torch.float16, 10 + replay), kept)
+        want = sp.wgrad(kept, d, km).clone()
+        wide = sp.wgrad(sp.q8_pack(_values(km.n_in, 40 + 8 * replay, torch.float16, 3)), _values(km.n_out, 64, torch.float16, 4), km)
+        small = sp.wgrad(sp.q8_pack(_values(other.n_in, 24, torch.float16, 5)), _values(other.n_out, 16, torch.float16, 6), other)
+        assert torch.isfinite(wide).all()
+        before = small.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(small, before)

@@ -267,3 +267,55 @@ def test_replays_in_a_hip_graph():
         torch.cuda.synchronize()
         for g, outs in graphs:
             assert all(torch.equal(a, c) for a, c in zip(outs, want)), replay
+
+
+@pytest.mark.parametrize("c", [5, 45, 96, 600, 2050])
+def test_backward_in_place(c):
+    """The C call lets dx be dout."""
+    import ctypes as C
+
+    import paper_2311_12862_amd as sp
+    x, dout = _rows(203, c, torch.float16, 1), _rows(203, c, torch.float16, 2)
+    w, b = _params(c, 3)
+    y, stats = sp.layer_norm_fwd(x, w, b, relu=True)
+    want = sp.layer_norm_bwd(dout, x, stats, w, gate=y)
+    lib = sp.load_library()
+    ws = torch.empty(lib.spconv_layer_norm_bwd_workspace(203, c), dtype=torch.int8, device="cuda")
+    dw, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+    stream = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert lib.spconv_layer_norm_bwd(p(dout), p(x), None, p(y), None, p(w), p(stats), 203, c, 1, p(dout), None, p(dw), p(db), p(ws),
+                                     ws.numel(), stream) == 0
+    assert torch.equal(dout, want[0]) and torch.equal(dw, want[1]) and torch.equal(db, want[2])
+
+
+def test_two_threads_on_two_streams():
+    import threading
+
+    import paper_2311_12862_amd as sp
+    inputs = [(_rows(30_001, 64, torch.float16, s), _rows(30_001, 64, torch.float16, s + 10)) for s in range(2)]
+    w, b = _params(64, 3)
+
+    def step(x, dout):
+        kept = sp.Checkpoint.empty(*x.shape)
+        y, stats = sp.layer_norm_fwd(x, w, b, relu=True, keep_x=kept)
+        return (y, *sp.layer_norm_bwd(dout, kept, stats, w, gate=y, residual=True))
+
+    want = [step(*i) for i in inputs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(40):
+                got = step(*inputs[k])
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(a, c) for a, c in zip(got, want[k])):
+                    wrong.append(k)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
