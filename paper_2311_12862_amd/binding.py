@@ -409,8 +409,8 @@ def _wgrad_q8(kept, dout, kmap, cfg, out, stream):
         out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
     else:
         _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
-    status = _LIB.spconv_wgrad_q8(kept.byref, _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
-                                  _stream(stream))
+    status = _LIB.spconv_wgrad_q8(kept.byref, dout.data_ptr() or None, kmap.handle, c_in, c_out, dt, _cfg(cfg), out.data_ptr(),
+                                  _stream_on(stream, dev))
     if status:
         _check(status, "spconv_wgrad_q8")
     return out
@@ -489,8 +489,11 @@ def _relu_bwd_q8(op, a, kept, out, stream):
             return _relu_bwd_q8(op, a, kept, out, stream)
     if out is None:
         out = torch.empty_like(a)
-    status = (_LIB or load_library()).spconv_relu_bwd_q8(_ptr(a), ref, _like(out, a, shape, dev), kept.rows * kept.channels, dt,
-                                                         _stream(stream))
+        to = out.data_ptr() or None
+    else:
+        to = _like(out, a, shape, dev)
+    status = (_LIB or load_library()).spconv_relu_bwd_q8(a.data_ptr() or None, ref, to, kept.rows * kept.channels, dt,
+                                                         _stream_on(stream, dev))
     if status:
         _check(status, "spconv_relu_bwd_q8")
     return out
@@ -511,12 +514,22 @@ def copy_cols(src, src_off: int, dst, dst_off: int, cols: int, stream=None):
 # A call of these takes 6 to 14 us on the host (two of each three go to torch's allocations and the launches), more than many of
 # their kernels: checks read a tensor's attributes once, and the device is switched only where it is another one.
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _device_now():
     """Number of the current device (a look-up, as in _current_stream)."""
     global _device_now
     torch.cuda.current_device()   # (initialises the device if nothing has yet)
     _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     return _device_now()
+
+
+def _stream_on(stream, dev):
+    """_stream for a call whose device is known to be the current one."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
 
 
 def _row_args(x):
@@ -622,8 +635,8 @@ def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     rows, channels = shape
     if out is None:
         out = Checkpoint.empty(rows, channels)
-    status = (_LIB or load_library()).spconv_q8_pack(_ptr(x), rows, channels, dt, _kept_like(out, x, shape, dev),
-                                                     _stream(stream))
+    status = (_LIB or load_library()).spconv_q8_pack(x.data_ptr() or None, rows, channels, dt, _kept_like(out, x, shape, dev),
+                                                     _stream_on(stream, dev))
     if status:
         _check(status, "spconv_q8_pack")
     return out
@@ -643,7 +656,8 @@ def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
         out = kept._data.new_empty((rows, channels), dtype=dtype)
     else:
         _out_tensor(out, (rows, channels), dtype, kept)
-    status = (_LIB or load_library()).spconv_q8_unpack(kept.byref, rows, channels, dt, _ptr(out), _stream(stream))
+    status = (_LIB or load_library()).spconv_q8_unpack(kept.byref, rows, channels, dt, out.data_ptr() or None,
+                                                       _stream_on(stream, dev))
     if status:
         _check(status, "spconv_q8_unpack")
     return out
@@ -666,10 +680,13 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     kept_y = None if keep_y is None else _kept_like(keep_y, x, shape, dev)
     if out is None:
         out = torch.empty_like(x)
-    y = _like(out, x, shape, dev)
+        y = out.data_ptr() or None
+    else:
+        y = _like(out, x, shape, dev)
     stats = x.new_empty((rows, 2), dtype=torch.float32)
     status = (_LIB or load_library()).spconv_layer_norm_fwd(
-        _ptr(x), res, w, b, eps, 1 if relu else 0, rows, channels, dt, y, _ptr(stats), kept_x, kept_y, _stream(stream))
+        x.data_ptr() or None, res, w, b, eps, 1 if relu else 0, rows, channels, dt, y, stats.data_ptr() or None, kept_x, kept_y,
+        _stream_on(stream, dev))
     if status:
         _check(status, "spconv_layer_norm_fwd")
     return out, stats
@@ -716,9 +733,10 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
         dbias = stats.new_empty((channels,))
         workspace = stats.new_empty((need // 4,))
         dw_ptr, db_ptr, ws_ptr = dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr()
-    st = _stream(stream)
-    status = lib.spconv_layer_norm_bwd(_ptr(dout), x_ptr, kept_x, y_ptr, kept_y, w, stats_ptr, rows, channels, dt, _ptr(dx),
-                                       None if dres is None else _ptr(dres), dw_ptr, db_ptr, ws_ptr, need, st)
+    st = _stream_on(stream, dev)
+    status = lib.spconv_layer_norm_bwd(dout.data_ptr() or None, x_ptr, kept_x, y_ptr, kept_y, w, stats_ptr, rows, channels, dt,
+                                       dx.data_ptr() or None, None if dres is None else dres.data_ptr() or None, dw_ptr, db_ptr,
+                                       ws_ptr, need, st)
     if status:
         _check(status, "spconv_layer_norm_bwd")
     if workspace is not None and stream is not None and st != _stream(None):
