@@ -374,7 +374,7 @@ SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual_or_null
                                      void* y, float* stats_or_null, const spconv_q8* keep_x_or_null,
                                      const spconv_q8* keep_y_or_null, void* stream);
 
-/* Bytes of the workspace that spconv_layer_norm_bwd needs for dweight and dbias (SPCONV_EINVAL for sizes it refuses). */
+/* Bytes of the workspace that spconv_layer_norm_bwd needs for dweight and dbias; 0: none (SPCONV_EINVAL for sizes it refuses). */
 SPCONV_API int64_t spconv_layer_norm_bwd_workspace(int64_t rows, int C);
 
 /* Gradients of spconv_layer_norm_fwd:
@@ -388,7 +388,7 @@ SPCONV_API int64_t spconv_layer_norm_bwd_workspace(int64_t rows, int C);
  *   dresidual        device [rows][C], or NULL
  *   dweight, dbias   device fp32 [C], fully overwritten, or both NULL
  *   workspace        device, at least spconv_layer_norm_bwd_workspace(rows, C) bytes, 16-byte aligned, for this call alone until it is
- *                    done; unused (may be NULL) without dweight
+ *                    done; unused (may be NULL) without dweight, or where that is 0
  * Sums are fp32 in a fixed order: the same call gives the same bits.  rows = 0 gives zero dweight and dbias.  EINVAL as above. */
 SPCONV_API int spconv_layer_norm_bwd(const void* dout, const void* x_or_null, const spconv_q8* kept_x_or_null,
                                      const void* y_or_null, const spconv_q8* kept_y_or_null, const float* weight_or_null,

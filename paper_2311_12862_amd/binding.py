@@ -692,9 +692,6 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     return out, stats
 
 
-_bwd_workspace = {}   # channels: bytes
-
-
 def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = False, affine: bool = True, stream=None):
     """spconv_layer_norm_bwd: (dx, dweight, dbias, dresidual) for a layer_norm_fwd that left stats.  x: its input or the
     Checkpoint of it; gate: its output or the Checkpoint of it where it had a ReLU.  dweight and dbias are fp32 [channels]
@@ -723,16 +720,15 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
     dweight = dbias = dw_ptr = db_ptr = workspace = ws_ptr = None
     need = 0
     if affine:
-        need = _bwd_workspace.get(channels)
-        if need is None:
-            need = lib.spconv_layer_norm_bwd_workspace(0, channels)
-            if need < 0:
-                _check(need, "spconv_layer_norm_bwd_workspace")
-            _bwd_workspace[channels] = need
+        need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
+        if need < 0:
+            _check(need, "spconv_layer_norm_bwd_workspace")
         dweight = stats.new_empty((channels,))
         dbias = stats.new_empty((channels,))
-        workspace = stats.new_empty((need // 4,))
-        dw_ptr, db_ptr, ws_ptr = dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr()
+        dw_ptr, db_ptr = dweight.data_ptr(), dbias.data_ptr()
+        if need:
+            workspace = stats.new_empty((need // 4,))
+            ws_ptr = workspace.data_ptr()
     st = _stream_on(stream, dev)
     status = lib.spconv_layer_norm_bwd(dout.data_ptr() or None, x_ptr, kept_x, y_ptr, kept_y, w, stats_ptr, rows, channels, dt,
                                        dx.data_ptr() or None, None if dres is None else dres.data_ptr() or None, dw_ptr, db_ptr,

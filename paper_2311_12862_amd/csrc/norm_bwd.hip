@@ -26,7 +26,9 @@ struct BwdArgs {
   const float2* stats;
   void* dx;
   void* dres;          // or null
-  float* partial;      // [workgroup][2][C], or null: no dw and db
+  float* dw;           // sums of workgroup g at dw + g * step and db + g * step, or null: none
+  float* db;
+  int step;
   long long rows;
   int C, nb;
 };
@@ -149,16 +151,17 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
     }
     if constexpr (kAhead) a = next;
   }
-  if (!p.partial) return;
+  if (!p.dw) return;
+  float* const to_w = p.dw + (long long)blockIdx.x * p.step;
+  float* const to_b = p.db + (long long)blockIdx.x * p.step;
   if constexpr (L == 256) {  // a lane's columns are its own
-    float* to = p.partial + (long long)blockIdx.x * 2 * C;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int i = 0; i < W; ++i)
         if (at[v].live && i >= at[v].lo) {
-          to[at[v].col + i] = dw[v][i];
-          to[C + at[v].col + i] = db[v][i];
+          to_w[at[v].col + i] = dw[v][i];
+          to_b[at[v].col + i] = db[v][i];
         }
   } else {
     static_assert(NV == 1, "");
@@ -184,7 +187,7 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
       float t = sums[which][0][c];
 #pragma unroll
       for (int k = 1; k < M; ++k) t += sums[which][k][c];
-      if (of.live && c % W >= of.lo) p.partial[((long long)blockIdx.x * 2 + which) * C + (of.col + c % W)] = t;
+      if (of.live && c % W >= of.lo) (which ? to_b : to_w)[of.col + c % W] = t;
     }
   }
 }
@@ -212,14 +215,31 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float* __restrict__ par
 
 constexpr int kBwdGroups = 1024;  // workgroups at most: four a CU, as registers allow (300k rows: 512 157 us, 1024 113, 2048 124)
 
-template <typename T> int launch_bwd(const BwdArgs& a, float* dw, float* db, hipStream_t st) {
-  return with_lanes<Row<T>::W>(a.C, [&](auto l) {
+// One workgroup for so few elements (counted with the idle lanes) that a second launch - 4 us on the host with its workspace, 4 to 5 on the
+// GPU - costs more than the wait for one row after the other, up to 16 turns of 0.5 to 0.9 us; it writes dw and db itself.  A call, us, one
+// workgroup and more: 8k elements 11.2, 15.8; 16k f16 of 256 11.1, 15.8; fp32 of 256 12.0, 15.9; 32k fp32 of 64 20, 16.
+constexpr int64_t kBwdAlone = 16384;
+bool alone(int64_t rows, int C) {
+  int wide = 32;
+  while (wide < C) wide *= 2;
+  return rows * wide <= kBwdAlone;
+}
+
+// a.dw, a.db: where the sums go in the end, or null
+template <typename T> int launch_bwd(const BwdArgs& args, float* workspace, hipStream_t st) {
+  return with_lanes<Row<T>::W>(args.C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    const int groups = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(a.rows, 256 / L), kBwdGroups));
+    const int groups = alone(args.rows, args.C) ? 1 : (int)std::min<int64_t>(ceil_div(args.rows, 256 / L), kBwdGroups);
+    BwdArgs a = args;
+    if (args.dw && !alone(args.rows, args.C)) {
+      a.dw = workspace;
+      a.db = workspace + args.C;
+      a.step = 2 * args.C;
+    }
     hipLaunchKernelGGL((k_norm_bwd<T, L, NV, decltype(l)::TAIL>), dim3((unsigned)groups), dim3(256), 0, st, a);
     SPC_LAUNCH_CHECK();
-    if (!a.partial) return (int)SPCONV_OK;
-    hipLaunchKernelGGL(k_norm_sum, dim3((unsigned)ceil_div(2 * a.C, 16)), dim3(1024), 0, st, a.partial, groups, a.C, dw, db);
+    if (a.dw == args.dw) return (int)SPCONV_OK;
+    hipLaunchKernelGGL(k_norm_sum, dim3((unsigned)ceil_div(2 * a.C, 16)), dim3(1024), 0, st, workspace, groups, a.C, args.dw, args.db);
     SPC_LAUNCH_CHECK();
     return (int)SPCONV_OK;
   });
@@ -234,7 +254,7 @@ extern "C" {
 
 SPCONV_API int64_t spconv_layer_norm_bwd_workspace(int64_t rows, int C) {
   if (!row_shape_ok(rows, C)) return SPCONV_EINVAL;
-  return (int64_t)kBwdGroups * 2 * C * (int64_t)sizeof(float);
+  return alone(rows, C) ? 0 : (int64_t)kBwdGroups * 2 * C * (int64_t)sizeof(float);
 }
 
 SPCONV_API int spconv_layer_norm_bwd(const void* dout, const void* x, const spconv_q8* kept_x, const void* y, const spconv_q8* kept_y,
@@ -242,7 +262,8 @@ SPCONV_API int spconv_layer_norm_bwd(const void* dout, const void* x, const spco
                                      void* dresidual, float* dweight, float* dbias, void* workspace, int64_t workspace_bytes,
                                      void* stream) {
   if (!row_shape_ok(rows, C) || !dtype_known(dtype) || !dweight != !dbias || (x && kept_x) || (y && kept_y)) return SPCONV_EINVAL;
-  if (dweight && (!workspace || workspace_bytes < spconv_layer_norm_bwd_workspace(rows, C))) return SPCONV_EINVAL;
+  const int64_t need = spconv_layer_norm_bwd_workspace(rows, C);
+  if (dweight && need > 0 && (!workspace || workspace_bytes < need)) return SPCONV_EINVAL;
   if (rows > 0 && (!dout || (!x && !kept_x) || !stats || !dx)) return SPCONV_EINVAL;
   if (rows > 0 && ((kept_x && !(kept_x->data && kept_x->exps)) || (kept_y && !(kept_y->data && kept_y->exps)))) return SPCONV_EINVAL;
   if (rows == 0 && !dweight) return SPCONV_OK;
@@ -256,15 +277,16 @@ SPCONV_API int spconv_layer_norm_bwd(const void* dout, const void* x, const spco
   a.stats = (const float2*)stats;
   a.dx = dx;
   a.dres = dresidual;
-  a.partial = dweight ? (float*)workspace : nullptr;
+  a.dw = dweight;
+  a.db = dbias;
   a.rows = rows;
   a.C = C;
   a.nb = (C + kQ8Block - 1) / kQ8Block;
   hipStream_t st = (hipStream_t)stream;
   switch (dtype) {
-    case SPCONV_F32: return launch_bwd<float>(a, dweight, dbias, st);
-    case SPCONV_F16: return launch_bwd<_Float16>(a, dweight, dbias, st);
-    case SPCONV_BF16: return launch_bwd<__bf16>(a, dweight, dbias, st);
+    case SPCONV_F32: return launch_bwd<float>(a, (float*)workspace, st);
+    case SPCONV_F16: return launch_bwd<_Float16>(a, (float*)workspace, st);
+    case SPCONV_BF16: return launch_bwd<__bf16>(a, (float*)workspace, st);
   }
   return SPCONV_EINVAL;
 }

@@ -116,6 +116,14 @@ def test_backward_variants(dtype, affine, relu, residual, kept, grads):
         _check_bwd(rows, c, dtype, affine, relu, residual, kept, shift, grads)
 
 
+@pytest.mark.parametrize("dtype", DTS)
+@pytest.mark.parametrize("rows,c", [(512, 32), (513, 32), (128, 100), (129, 100), (4, 4096), (5, 4096), (512, 8), (513, 3)])
+def test_backward_around_one_workgroup(dtype, rows, c):
+    """As many rows as one workgroup takes alone, and one more."""
+    for kept in (0, 2):
+        _check_bwd(rows, c, dtype, True, True, True, kept)
+
+
 @pytest.mark.parametrize("dtype,c", [(torch.float16, 32), (torch.bfloat16, 256), (torch.float32, 45)])
 def test_many_rows(dtype, c):
     _check_fwd(150_001, c, dtype, True, True, True)
@@ -275,7 +283,7 @@ def test_backward_in_place(c):
     import ctypes as C
 
     import paper_2311_12862_amd as sp
-    x, dout = _rows(203, c, torch.float16, 1), _rows(203, c, torch.float16, 2)
+    x, dout = _rows(203, c, torch.float16, 1), _rows(203, c, torch.float16, 2)   # (one workgroup at c = 5 and 45)
     w, b = _params(c, 3)
     y, stats = sp.layer_norm_fwd(x, w, b, relu=True)
     want = sp.layer_norm_bwd(dout, x, stats, w, gate=y)

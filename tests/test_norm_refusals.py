@@ -53,11 +53,11 @@ def test_null_pointers(lib):
 
 
 def test_backward_arguments(lib):
-    need = lib.spconv_layer_norm_bwd_workspace(4, 8)
-    assert need > 0
+    need = lib.spconv_layer_norm_bwd_workspace(4000, 8)
+    assert need > 0 and lib.spconv_layer_norm_bwd_workspace(4, 8) == 0
 
     def bwd(dout=P, x=P, kx=None, y=None, ky=None, stats=P, dx=P, dw=P, db=P, ws=P, n=need):
-        return lib.spconv_layer_norm_bwd(dout, x, kx, y, ky, None, stats, 4, 8, 1, dx, None, dw, db, ws, n, None)
+        return lib.spconv_layer_norm_bwd(dout, x, kx, y, ky, None, stats, 4000, 8, 1, dx, None, dw, db, ws, n, None)
 
     assert bwd(dout=None) == EINVAL and bwd(x=None) == EINVAL and bwd(stats=None) == EINVAL and bwd(dx=None) == EINVAL
     assert bwd(kx=_q8()) == EINVAL                       # both inputs
