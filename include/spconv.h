@@ -353,8 +353,9 @@ SPCONV_API int spconv_q8_unpack(const spconv_q8* kept, int64_t rows, int C, spco
 SPCONV_API int spconv_relu_bwd_q8(const void* dout, const spconv_q8* kept, void* out, int64_t n, spconv_dtype dtype, void* stream);
 
 /* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout.  The values are exact in dtype: the result is
- * that of spconv_wgrad on the unpacked tensor.  16-bit layers of C_in % 16 == 0 on kmaps of K < 5 gather data itself where it is 16-byte
- * aligned; others unpack it first, into memory that the kmap then keeps (one call before a capture makes it). */
+ * that of spconv_wgrad on the unpacked tensor.  16-bit layers on kmaps of K < 5 gather data itself where it is 4-byte aligned
+ * (narrow ones on dense maps, whose gradient comes from the map, do not); others unpack it first, into memory that the kmap then keeps (one
+ * call before a capture makes it). */
 SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
                                const spconv_config* cfg_or_null, float* dweights, void* stream);
 

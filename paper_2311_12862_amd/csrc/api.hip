@@ -754,7 +754,7 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
   hipStream_t st = (hipStream_t)stream;
   spconv_config c;
   SPC_TRY(resolve_config(cfg, dtype, &c));
-  if (wgrad_takes_q8(km, kept, C_in, dtype)) {
+  if (wgrad_takes_q8(km, kept, dtype)) {
     km->last_stream = st;
     bool from_map;
     SPC_TRY(wgrad_route(km, C_in, C_out, dtype, c, st, &from_map));

@@ -739,10 +739,10 @@ int64_t wgrad_auto_pairs(const spconv_kmap* km, int C_in, int C_out, spconv_dtyp
 }
 
 // Whether a checkpoint is gathered as it is (wgrad_q8.hip, with both sides measured: it is ahead of unpacking on all but a few
-// shapes, and there within 6 %); else it is unpacked first: fp32 layers, whose gradient the matrix instructions bound, rows that are no
-// whole 16-byte pieces, and the planes of a K = 5 map, which would each convert their pairs.
-bool wgrad_takes_q8(const spconv_kmap* km, const spconv_q8* kept, int C_in, spconv_dtype dtype) {
-  return dtype != SPCONV_F32 && C_in % 16 == 0 && ((size_t)kept->data & 15) == 0 && km->groups.empty();
+// shapes, and there within 6 %); else it is unpacked first: fp32 layers, whose gradient the matrix instructions bound, data at an
+// address that is no multiple of 4, and the planes of a K = 5 map, which would each convert their pairs.
+bool wgrad_takes_q8(const spconv_kmap* km, const spconv_q8* kept, spconv_dtype dtype) {
+  return dtype != SPCONV_F32 && ((size_t)kept->data & 3) == 0 && km->groups.empty();
 }
 
 // piece_pairs: pairs of a piece, 0: chosen here.  kept: in the place of feats

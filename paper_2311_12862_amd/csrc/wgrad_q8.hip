@@ -4,7 +4,8 @@
 // A pair's row of x is C_in bytes and an exponent for every 32 of them instead of 2 C_in.  Rows go straight into LDS as they are;
 // every lane then turns the 16 channels that it loaded itself into the layer's type, once per batch and workgroup (fragments are
 // read by several waves: turning them there would cost four times the instructions), and writes them where the transposing
-// reads expect them.  x therefore runs a batch ahead of dy.
+// reads expect them.  x therefore runs a batch ahead of dy.  (Where C_in ends inside a piece of 16, the rest of it is the next row's or, past
+// the buffer, whose range is checked by the dword, zero: channels of dW that are not there to be stored.)
 //
 // Up to 128 channels a workgroup's waves go through a batch together and three workgroups share a CU (one converted batch, a barrier
 // before it is replaced: with two of them and two workgroups 2.45M pairs 256 -> 64 took 310 us, so 239).  The 256 x 256 tile

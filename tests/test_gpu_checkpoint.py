@@ -205,7 +205,8 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(sp.ew(sp.EW_RELU_BWD, out, kept)[-3000:], out[-3000:].relu())
 
 
-@pytest.mark.parametrize("ci,co", [(16, 16), (32, 32), (48, 64), (64, 64), (96, 96), (80, 40), (112, 128), (256, 256), (400, 72)])
+@pytest.mark.parametrize("ci,co", [(8, 16), (16, 16), (24, 8), (32, 32), (40, 64), (48, 64), (64, 64), (72, 96), (96, 96), (80, 40),
+                                   (104, 128), (112, 128), (200, 136), (256, 256), (264, 200), (400, 72)])
 @pytest.mark.parametrize("dtype", DTS)
 @pytest.mark.parametrize("kind", ["sub3", "down", "dense"])
 def test_wgrad_has_the_bits_of_the_unpacked_tensor(ci, co, dtype, kind):
@@ -245,7 +246,7 @@ def test_wgrad_captured_then_a_larger_layer():
     """A captured call that unpacks replays on its own room after a wider layer of the kmap took a larger one."""
     import paper_2311_12862_amd as sp
     km, other = _map("sub3"), _map("sub3", 1500)
-    x, d = _values(km.n_in, 24, torch.float16, 1), _values(km.n_out, 16, torch.float16, 2)
+    x, d = _values(km.n_in, 24, torch.float32, 1), _values(km.n_out, 16, torch.float32, 2)
     kept = sp.q8_pack(x)
     sp.wgrad(kept, d, km)
     torch.cuda.synchronize()
@@ -253,10 +254,10 @@ def test_wgrad_captured_then_a_larger_layer():
     with torch.cuda.graph(graph):
         got = sp.wgrad(kept, d, km)
     for replay in range(3):
-        sp.q8_pack(_values(km.n_in, 24, torch.float16, 10 + replay), kept)
+        sp.q8_pack(_values(km.n_in, 24, torch.float32, 10 + replay), kept)
         want = sp.wgrad(kept, d, km).clone()
-        wide = sp.wgrad(sp.q8_pack(_values(km.n_in, 40 + 8 * replay, torch.float16, 3)), _values(km.n_out, 64, torch.float16, 4), km)
-        small = sp.wgrad(sp.q8_pack(_values(other.n_in, 24, torch.float16, 5)), _values(other.n_out, 16, torch.float16, 6), other)
+        wide = sp.wgrad(sp.q8_pack(_values(km.n_in, 40 + 8 * replay, torch.float32, 3)), _values(km.n_out, 64, torch.float32, 4), km)
+        small = sp.wgrad(sp.q8_pack(_values(other.n_in, 24, torch.float32, 5)), _values(other.n_out, 16, torch.float32, 6), other)
         assert torch.isfinite(wide).all()
         before = small.clone()
         graph.replay()
