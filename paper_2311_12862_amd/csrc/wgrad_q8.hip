@@ -14,7 +14,7 @@
 //
 // bf16, 2.45M pairs of 300k rows, us for both kernels of a call, unpacking first and directly: 64 -> 64 100, 89; 96 -> 96 180, 162;
 // 128 -> 128 218, 178; 256 -> 64 315, 239; 64 -> 256 (x is gathered for two column tiles) 290, 292; 256 -> 256 400, 360.
-// 380k pairs of 100k rows: 64 -> 64 29.5, 22.9; 96 -> 96 40.6, 43.1; 128 -> 128 47.4, 45.5; 113k pairs 32 -> 32 14.7, 11.7.
+// 380k pairs of 100k rows: 64 -> 64 29.5, 22.9; 96 -> 96 41.1, 41.1; 128 -> 128 47.5, 44.4; 113k pairs 32 -> 32 14.7, 11.7.
 #include "wgrad.h"
 #include "rows.h"
 
@@ -227,17 +227,23 @@ __global__ void __launch_bounds__(NWI* NWO* NWK * 64) k_wgrad_q8(const WgradPara
       qb[i] = *reinterpret_cast<const unsigned*>(my + W::at_b + slot * W::b_stage + (wave * CH + i) * 256 + lane * 4);
     }
   };
-  auto convert = [&](int c) {
+  u32x4 wide[CH][2];
+  auto widen = [&]() {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      u32x4 v[2];
-      widen16<T>(q[i], qb[i], v);
+    for (int i = 0; i < CH; ++i) widen16<T>(q[i], qb[i], wide[i]);
+  };
+  auto put = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
       if (kWhole || x_to[i] >= 0) {
         u32x4* to = reinterpret_cast<u32x4*>(my + W::at_x + c * W::x_bytes + x_to[i]);
-        to[0] = v[0];
-        to[1] = v[1];
+        to[0] = wide[i][0];
+        to[1] = wide[i][1];
       }
-    }
+  };
+  auto convert = [&](int c) {
+    widen();
+    put(c);
   };
   auto sync = [&]() {
     if constexpr (NW > 1) asm volatile("s_barrier" ::: "memory");
@@ -380,11 +386,16 @@ __global__ void __launch_bounds__(NWI* NWO* NWK * 64) k_wgrad_q8(const WgradPara
         for (int o = 0; o < OB; ++o) acc[o][i] = mma<T>(d[o], x[i], acc[o][i]);
         x[i] = frag(xs + xa[i], TI * 2);
       }
+      widen();  // batch b + 2, before everyone waits
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(wide[i][j]));
       if constexpr (NW > 1) {  // everyone has read batch b + 1 (one wave's accesses keep their order)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         sync();
       }
-      convert(0);  // batch b + 2
+      put(0);
 #pragma unroll
       for (int o = 0; o < OB; ++o) d[o] = dn[o];
     }
