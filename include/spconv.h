@@ -333,7 +333,7 @@ SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km
  * value over the step 2^(b - 133), rounded to nearest even, at most 127 in magnitude, and +-1 where a value other than 0 would round
  * to 0.  So a value is off by at most half a step - one step where it is kept from rounding to 128 or to 0 - which is
  * 2^-7 (2^-6) of the block's largest magnitude; its sign is always right.  A block with an infinity or a NaN has b = 255 and
- * q = 0, and stands for NaN throughout.
+ * q = 0, and stands for NaN throughout (b = 255 does, whatever q is).
  * Both pointers belong to the caller and need no alignment; C is 1 to 4096, rows * C at most 2^40.  Rows with a large offset
  * (|mean| far above the spread) lose their spread to it: the step goes by the largest magnitude. */
 typedef struct spconv_q8 {
@@ -367,9 +367,10 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
  *   relu             0 or 1: act(v) = v < 0 ? 0 : v (a NaN stays a NaN)
  *   stats            device fp32 [rows][2] receives (m, r) of each row for the backward pass; may be NULL
  *   keep_x, keep_y   receive checkpoints of x and of y (as written) in the same pass: what spconv_q8_pack makes of them;
- *                    each may be NULL
- * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  mean + eps counts as 2^-126 where it is less.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
- * `stream` and allocates nothing.  EINVAL: null pointers, sizes, dtype, relu, eps negative or NaN. */
+ *                    each may be NULL, in memory of its own
+ * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  mean((x - m)^2) + eps counts as 2^-126 where it is less.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
+ * `stream` and allocates nothing.  EINVAL: null pointers, sizes, dtype, relu, eps negative or NaN, one place for
+ * two checkpoints. */
 SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual_or_null, const float* weight_or_null,
                                      const float* bias_or_null, float eps, int relu, int64_t rows, int C, spconv_dtype dtype,
                                      void* y, float* stats_or_null, const spconv_q8* keep_x_or_null,

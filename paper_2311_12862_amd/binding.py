@@ -596,9 +596,9 @@ class Checkpoint:
         at = (rows * channels + 15) // 16 * 16
         self._data = torch.empty((at + rows * (-(-channels // 32)),), dtype=torch.int8, device=device)
         self._exps = at
+        if not self._data.is_cuda:
+            raise ValueError(f"expected a device, got {device}")
         base = self._data.data_ptr()
-        if base == 0 and rows:
-            raise ValueError("expected a contiguous device tensor")
         self.byref = C.byref(Q8(base or None, base + at or None))
         return self
 

@@ -135,6 +135,7 @@ SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual, const 
   if (!row_shape_ok(rows, C) || !dtype_known(dtype) || !(eps >= 0.f) || relu < 0 || relu > 1) return SPCONV_EINVAL;
   if (rows == 0) return SPCONV_OK;
   if (!x || !y || (keep_x && !(keep_x->data && keep_x->exps)) || (keep_y && !(keep_y->data && keep_y->exps))) return SPCONV_EINVAL;
+  if (keep_x && keep_y && (keep_x->data == keep_y->data || keep_x->exps == keep_y->exps)) return SPCONV_EINVAL;
   FwdArgs a{};
   a.x = x;
   a.res = residual;

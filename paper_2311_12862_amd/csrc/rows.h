@@ -133,10 +133,10 @@ struct Q8Ref {  // a checkpoint: [rows][C] and [rows][ceil(C / 32)]
   unsigned char* b;
 };
 
-// 2^(b - 133) (subnormal for the smallest b); infinite for b = 255, which turns q = 0 into a NaN
+// 2^(b - 133) (subnormal for the smallest b); a NaN for b = 255
 __device__ __forceinline__ float q8_step(unsigned b) {
   const float s = ldexpf(1.f, (int)b - 133);
-  return b == 255u ? __builtin_inff() : s;
+  return b == 255u ? __builtin_nanf("") : s;
 }
 template <int W> struct Bytes;  // the q of a vector
 template <> struct Bytes<8> { typedef raw8 word; };

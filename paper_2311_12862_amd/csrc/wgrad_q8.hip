@@ -33,8 +33,8 @@ __device__ __forceinline__ void load_byte_to_lds(u32x4 rsrc, unsigned voff, unsi
 template <typename T> __device__ __forceinline__ void widen16(u32x4 q, unsigned b, u32x4 (&out)[2]);
 template <> __device__ __forceinline__ void widen16<_Float16>(u32x4 q, unsigned b, u32x4 (&out)[2]) {
   // a byte q + 128 as the low bits of a half in [16, 32): 16 + (q + 128) / 64.  Less 18 that is q / 64, times 2^(b - 127): the factor
-  // is a half (subnormal down to 2^-24) for all that a half can be, zero below and infinite above, where q = 0 makes a NaN of it.
-  const _Float16 s = (_Float16)__builtin_bit_cast(float, b << 23);
+  // is a half (subnormal down to 2^-24) for all that a half can be, zero below and infinite above.
+  const _Float16 s = (_Float16)(b == 255u ? __builtin_nanf("") : __builtin_bit_cast(float, b << 23));
   const f16x2 scale = {s, s}, less = {(_Float16)-18.f, (_Float16)-18.f};
 #pragma unroll
   for (int w = 0; w < 4; ++w) {

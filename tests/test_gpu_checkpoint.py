@@ -263,3 +263,50 @@ def test_wgrad_captured_then_a_larger_layer():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(small, before)
+
+
+@pytest.mark.parametrize("dtype", DTS)
+@pytest.mark.parametrize("rows,c", [(3, 7), (70, 45), (33, 64), (5, 1000)])
+def test_nothing_beside_a_checkpoint_is_written(dtype, rows, c):
+    import paper_2311_12862_amd as sp
+    nb = -(-c // 32)
+    for shift in (0, 1, 3, 4):
+        data = torch.full((rows * c + 16,), 99, dtype=torch.int8, device="cuda")
+        exps = torch.full((rows * nb + 16,), 99, dtype=torch.uint8, device="cuda")
+        kept = sp.Checkpoint(data[shift:shift + rows * c].view(rows, c), exps[shift:shift + rows * nb].view(rows, nb))
+        x = _values(rows, c, dtype, c)
+        sp.q8_pack(x, kept)
+        q, b = pack64(x)
+        _same(kept, (q, b))
+        again = sp.Checkpoint(data[shift:shift + rows * c].view(rows, c).zero_(), kept.exps.zero_())
+        sp.layer_norm_fwd(x, keep_x=again)
+        _same(again, (q, b))
+        for t, n in ((data, rows * c), (exps, rows * nb)):
+            assert (t[:shift] == 99).all() and (t[shift + n:] == 99).all()
+        assert torch.equal(sp.q8_unpack(kept, dtype).double(), unpack64(q, b))
+
+
+@pytest.mark.parametrize("dtype", DTS)
+def test_checkpoints_that_no_tensor_has(dtype):
+    """Any bytes are a checkpoint: q = -128, steps of every size, b = 255 a NaN whatever q is; every reader sees the same values."""
+    import paper_2311_12862_amd as sp
+    km = _map("one", 600)
+    n = km.n_in
+    g = torch.Generator(device="cuda").manual_seed(1)
+    data = torch.randint(-128, 128, (n, 64), generator=g, device="cuda").to(torch.int8)
+    exps = torch.randint(100, 140, (n, 2), generator=g, device="cuda").to(torch.uint8)
+    exps[7, 0] = 255
+    exps[9, 1] = 0
+    kept = sp.Checkpoint(data, exps)
+    want = unpack64(data, exps)
+    values = sp.q8_unpack(kept, dtype)
+    assert torch.isnan(values[7, :32]).all() and torch.equal(torch.isnan(values), torch.isnan(want))
+    within = ~torch.isnan(want) & (want.to(dtype).double() == want)
+    assert torch.equal(values.double()[within], want[within])
+    d = torch.zeros(n, 16, dtype=dtype, device="cuda")
+    d[11, 3], d[9, 4], d[30, 5] = 1, 1, 1
+    dw = sp.wgrad(kept, d, km)[0]
+    rows = torch.tensor([11, 9, 30], device="cuda")
+    got, fits = dw[:, 3:6].t().double(), within[rows]
+    # (a NaN times a zero is a NaN: channels of the block that has one)
+    assert torch.isnan(got[:, :32]).all() and torch.equal(got[:, 32:][fits[:, 32:]], want[rows][:, 32:][fits[:, 32:]])

@@ -327,3 +327,39 @@ def test_two_threads_on_two_streams():
     for t in threads:
         t.join()
     assert not wrong
+
+
+def test_one_of_weight_and_bias_and_no_statistics():
+    """Weights at odd addresses, one of the two alone, and the C call without statistics."""
+    import ctypes as C
+
+    import paper_2311_12862_amd as sp
+    for c in (45, 64):
+        x = _rows(100, c, torch.float16, c)
+        w, b = (_shifted(t, 1 + i)[0] for i, t in enumerate(_params(c, 7)))
+        for weight, bias in ((w, None), (None, b), (w, b)):
+            y, stats = sp.layer_norm_fwd(x, weight, bias, EPS)
+            want, _, tol, _ = fwd64(x, weight, bias, EPS, False, None)
+            within(y, want, tol, torch.float16)
+        p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
+        got = torch.empty_like(y)
+        assert sp.load_library().spconv_layer_norm_fwd(p(x), None, p(w), p(b), EPS, 0, 100, c, 1, p(got), None, None, None,
+                                                       C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+        assert torch.equal(got, y)
+        dout = _rows(100, c, torch.float16, 9)
+        values, tol = bwd64(dout, x, stats, w, None)
+        within(sp.layer_norm_bwd(dout, x, stats, w)[0], values[0], tol[0], torch.float16)
+
+
+def test_eps_of_zero_and_a_large_one():
+    """A row without variance has y = bias, not a NaN."""
+    import paper_2311_12862_amd as sp
+    x = torch.zeros(9, 40, device="cuda")
+    x[4:] = _rows(5, 40, torch.float32, 1)
+    w, b = _params(40, 2)
+    y, stats = sp.layer_norm_fwd(x, w, b, 0.0)
+    assert torch.isfinite(y).all() and torch.equal(y[:4], b.expand(4, 40))
+    dx, dw, db, _ = sp.layer_norm_bwd(torch.zeros_like(x), x, stats, w)
+    assert (dx == 0).all() and (dw == 0).all() and (db == 0).all()
+    y, _ = sp.layer_norm_fwd(x, w, b, 1e30)
+    assert (y - b).abs().max().item() < 1e-12 + 2 ** -24 * b.abs().max().item()

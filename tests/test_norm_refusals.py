@@ -49,6 +49,7 @@ def test_null_pointers(lib):
         k.get("x", P), None, None, None, k.get("eps", 1e-5), k.get("relu", 0), 4, 8, 1, k.get("y", P), P, k.get("kx"), k.get("ky"), None)
     assert fwd(x=None) == EINVAL and fwd(y=None) == EINVAL
     assert fwd(eps=-1e-6) == EINVAL and fwd(eps=float("nan")) == EINVAL and fwd(relu=2) == EINVAL and fwd(relu=-1) == EINVAL
+    assert fwd(kx=_q8(), ky=_q8(4096, 8192)) == EINVAL and fwd(kx=_q8(), ky=_q8(8192, 4096)) == EINVAL   # one place for two
     assert fwd(kx=_q8(None)) == EINVAL and fwd(kx=_q8(4096, None)) == EINVAL and fwd(ky=_q8(None)) == EINVAL
 
 
@@ -86,6 +87,10 @@ def test_binding_takes_device_tensors_only():
         sp.layer_norm_bwd(x, x, torch.zeros(4, 2))
     with pytest.raises(ValueError):
         sp.Checkpoint(torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        sp.Checkpoint.empty(4, 8, "cpu")
+    with pytest.raises(ValueError):
+        sp.Checkpoint.empty(4, 0)
 
 
 @pytest.mark.gpu
@@ -119,7 +124,7 @@ def test_binding_checks_shapes_and_types():
     with pytest.raises(ValueError):
         sp.layer_norm_bwd(x, x.half(), stats)
     for call in (lambda: sp.q8_pack(x, other), lambda: sp.q8_unpack(kept, torch.float32, x[:3]), lambda: sp.layer_norm_fwd(x, w[:39]),
-                 lambda: sp.layer_norm_fwd(x, keep_x=other), lambda: sp.layer_norm_fwd(x, out=x[:3]), lambda: sp.layer_norm_fwd(x, eps=-1.0),
+                 lambda: sp.layer_norm_fwd(x, keep_x=other), lambda: sp.layer_norm_fwd(x, keep_x=kept, keep_y=kept), lambda: sp.layer_norm_fwd(x, out=x[:3]), lambda: sp.layer_norm_fwd(x, eps=-1.0),
                  lambda: sp.layer_norm_bwd(x, other, stats), lambda: sp.layer_norm_bwd(x, x, stats, gate=other),
                  lambda: sp.layer_norm_bwd(x, x, stats[:3]), lambda: sp.layer_norm_bwd(x[:3], x, stats[:3])):
         with pytest.raises(sp.SpconvError):
