@@ -11,7 +11,7 @@ namespace {
 
 // Rows of C channels, a group of L lanes each; 256 / L rows of a workgroup, whose first is the same for all its lanes (addresses are a
 // scalar base and 32 bits per lane).
-template <typename T, int L, int NV, bool TAIL>
+template <typename T, int L, int NV, Ends E>
 __global__ void __launch_bounds__(256) k_q8_pack(const T* __restrict__ x, Q8Ref to, long long rows, int C, int nb) {
   constexpr int W = Row<T>::W, R = 256 / L;
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
@@ -25,16 +25,16 @@ __global__ void __launch_bounds__(256) k_q8_pack(const T* __restrict__ x, Q8Ref 
       const Place at = place_in_row<W>(v * L + lane, C);
       const bool live = row && at.live;
       raw16 raw = {};
-      if (live) raw = Row<T>::template load<TAIL>(xr + (rl * C + at.col), at, C);
+      if (live) raw = Row<T>::template load<E>(xr + (rl * C + at.col), at);
       float f[W];
       Row<T>::widen(raw, f);
-      own_only<TAIL>(at, f);
-      q8_keep<TAIL, L, W>(q + rl * C, b + rl * nb, at, live, f);
+      own_only<E>(at, f);
+      q8_keep<E, L, W>(q + rl * C, b + rl * nb, at, live, f);
     }
   }
 }
 
-template <typename T, int L, int NV, bool TAIL>
+template <typename T, int L, int NV, Ends E>
 __global__ void __launch_bounds__(256) k_q8_unpack(Q8Ref from, T* __restrict__ out, long long rows, int C, int nb) {
   constexpr int W = Row<T>::W, R = 256 / L;
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
@@ -47,10 +47,10 @@ __global__ void __launch_bounds__(256) k_q8_unpack(Q8Ref from, T* __restrict__ o
     for (int v = 0; v < NV; ++v) {
       const Place at = place_in_row<W>(v * L + lane, C);
       if (at.live) {
-        const auto w = q8_load<TAIL, W>(q + (rl * C + at.col), at, C);
+        const auto w = q8_load<E, W>(q + (rl * C + at.col), at);
         float f[W];
         q8_widen<W>(w, q8_step(b[rl * nb + at.block]), f);
-        Row<T>::template store<TAIL>(o + (rl * C + at.col), at, Row<T>::narrow(f));
+        Row<T>::template store<E>(o + (rl * C + at.col), at, Row<T>::narrow(f));
       }
     }
   }
@@ -91,7 +91,7 @@ template <typename T> int launch_pack(const void* x, long long rows, int C, cons
   blocks_as_rows(&rows, &C);
   return with_lanes<Row<T>::W>(C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    hipLaunchKernelGGL((k_q8_pack<T, L, NV, decltype(l)::TAIL>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, (const T*)x, to, rows, C,
+    hipLaunchKernelGGL((k_q8_pack<T, L, NV, decltype(l)::E>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, (const T*)x, to, rows, C,
                        (C + kQ8Block - 1) / kQ8Block);
     SPC_LAUNCH_CHECK();
     return (int)SPCONV_OK;
@@ -101,7 +101,7 @@ template <typename T> int launch_unpack(const Q8Ref& from, long long rows, int C
   blocks_as_rows(&rows, &C);
   return with_lanes<Row<T>::W>(C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    hipLaunchKernelGGL((k_q8_unpack<T, L, NV, decltype(l)::TAIL>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, from, (T*)out, rows, C,
+    hipLaunchKernelGGL((k_q8_unpack<T, L, NV, decltype(l)::E>), dim3(grid_for(rows, 256 / L)), dim3(256), 0, st, from, (T*)out, rows, C,
                        (C + kQ8Block - 1) / kQ8Block);
     SPC_LAUNCH_CHECK();
     return (int)SPCONV_OK;

@@ -26,7 +26,7 @@ struct FwdArgs {
   float eps;
 };
 
-template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds__(256) k_norm_fwd(const FwdArgs p) {
+template <typename T, int L, int NV, Ends E> __global__ void __launch_bounds__(256) k_norm_fwd(const FwdArgs p) {
   constexpr int W = Row<T>::W, R = 256 / L;
   __shared__ float part[2][4];
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
@@ -47,16 +47,16 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
       raw[v] = res[v] = raw16{0, 0, 0, 0};
       if (row && at[v].live) {
         const int e = rl * C + at[v].col;
-        raw[v] = Row<T>::template load<TAIL>((const T*)p.x + e0 + e, at[v], C);
-        if (p.res) res[v] = Row<T>::template load<TAIL>((const T*)p.res + e0 + e, at[v], C);
+        raw[v] = Row<T>::template load<E>((const T*)p.x + e0 + e, at[v]);
+        if (p.res) res[v] = Row<T>::template load<E>((const T*)p.res + e0 + e, at[v]);
       }
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       Row<T>::widen(raw[v], x[v]);
-      own_only<TAIL>(at[v], x[v]);
+      own_only<E>(at[v], x[v]);
       if (p.kept_x.q)
-        q8_keep<TAIL, L, W>(p.kept_x.q + e0 + rl * C, p.kept_x.b + r0 * p.nb + rl * p.nb, at[v], row && at[v].live, x[v]);
+        q8_keep<E, L, W>(p.kept_x.q + e0 + rl * C, p.kept_x.b + r0 * p.nb + rl * p.nb, at[v], row && at[v].live, x[v]);
 #pragma unroll
       for (int i = 0; i < W; ++i) sum += x[v][i];
     }
@@ -67,7 +67,7 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
       const float m = at[v].live ? mean : 0.f;
 #pragma unroll
       for (int i = 0; i < W; ++i) x[v][i] -= m;
-      own_only<TAIL>(at[v], x[v]);
+      own_only<E>(at[v], x[v]);
 #pragma unroll
       for (int i = 0; i < W; ++i) sq += x[v][i] * x[v][i];
     }
@@ -81,12 +81,12 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
 #pragma unroll
       for (int i = 0; i < W; ++i) y[i] = x[v][i] * rstd;
       if (p.w) {
-        if (live) load_floats<TAIL, W>(p.w + at[v].col, at[v], C, t);
+        if (live) load_floats<E, W>(p.w + at[v].col, at[v], t);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] *= t[i];
       }
       if (p.b) {
-        if (live) load_floats<TAIL, W>(p.b + at[v].col, at[v], C, t);
+        if (live) load_floats<E, W>(p.b + at[v].col, at[v], t);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] += t[i];
       }
@@ -100,12 +100,12 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
         for (int i = 0; i < W; ++i) y[i] = __builtin_elementwise_maximum(y[i], 0.f);  // (a NaN stays one)
       }
       const raw16 out = Row<T>::narrow(y);
-      if (live) Row<T>::template store<TAIL>((T*)p.y + e0 + (rl * C + at[v].col), at[v], out);
+      if (live) Row<T>::template store<E>((T*)p.y + e0 + (rl * C + at[v].col), at[v], out);
       if (p.kept_y.q) {  // of what was written
         Row<T>::widen(out, y);
 #pragma unroll
-        for (int i = 0; i < W; ++i) y[i] = live && (!TAIL || i >= at[v].lo) ? y[i] : 0.f;
-        q8_keep<TAIL, L, W>(p.kept_y.q + e0 + rl * C, p.kept_y.b + r0 * p.nb + rl * p.nb, at[v], live, y);
+        for (int i = 0; i < W; ++i) y[i] = live && (E == kWholeVectors || i >= at[v].lo) ? y[i] : 0.f;
+        q8_keep<E, L, W>(p.kept_y.q + e0 + rl * C, p.kept_y.b + r0 * p.nb + rl * p.nb, at[v], live, y);
       }
     }
   }
@@ -116,7 +116,7 @@ template <typename T> int launch_fwd(const FwdArgs& a, hipStream_t st) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
     // as many workgroups as the GPU holds (300k rows of 256 bf16: 85 us, with one workgroup per 256 / L rows 93)
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.rows, 256 / L), 2048);
-    hipLaunchKernelGGL((k_norm_fwd<T, L, NV, decltype(l)::TAIL>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_norm_fwd<T, L, NV, decltype(l)::E>), dim3(grid), dim3(256), 0, st, a);
     SPC_LAUNCH_CHECK();
     return (int)SPCONV_OK;
   });

@@ -53,7 +53,7 @@ template <int W> __device__ __forceinline__ raw16 raw_of(typename Bytes<W>::word
   return r;
 }
 
-template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds__(256) k_norm_bwd(const BwdArgs p) {
+template <typename T, int L, int NV, Ends E> __global__ void __launch_bounds__(256) k_norm_bwd(const BwdArgs p) {
   constexpr int W = Row<T>::W, R = 256 / L;
   constexpr bool kAhead = NV == 1;  // the next row is on its way while this one is worked on
   __shared__ float part[2][4];
@@ -67,7 +67,7 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
     at[v] = place_in_row<W>(v * L + lane, C);
 #pragma unroll
     for (int i = 0; i < W; ++i) w[v][i] = 1.f;
-    if (p.w && at[v].live) load_floats<TAIL, W>(p.w + at[v].col, at[v], C, w[v]);
+    if (p.w && at[v].live) load_floats<E, W>(p.w + at[v].col, at[v], w[v]);
   }
   // (the workgroup's first row r0 is the same for all its lanes: addresses are a scalar base and 32 bits per lane)
   auto load = [&](long long r0, BwdRow<NV>& a) {
@@ -81,15 +81,15 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
       a.b[v] = 0;
       if (row && at[v].live) {
         const int e = rl * C + at[v].col;
-        a.d[v] = Row<T>::template load<TAIL>((const T*)p.dout + e0 + e, at[v], C);
+        a.d[v] = Row<T>::template load<E>((const T*)p.dout + e0 + e, at[v]);
         if (p.x) {
-          a.x[v] = Row<T>::template load<TAIL>((const T*)p.x + e0 + e, at[v], C);
+          a.x[v] = Row<T>::template load<E>((const T*)p.x + e0 + e, at[v]);
         } else {
-          a.x[v] = raw_of<W>(q8_load<TAIL, W>(p.xq.q + e0 + e, at[v], C));
+          a.x[v] = raw_of<W>(q8_load<E, W>(p.xq.q + e0 + e, at[v]));
           a.b[v] = p.xq.b[r0 * p.nb + (rl * p.nb + at[v].block)];
         }
-        if (p.gate) a.y[v] = Row<T>::template load<TAIL>((const T*)p.gate + e0 + e, at[v], C);
-        else if (p.gate_q) a.y[v] = raw_of<W>(q8_load<TAIL, W>(p.gate_q + e0 + e, at[v], C));
+        if (p.gate) a.y[v] = Row<T>::template load<E>((const T*)p.gate + e0 + e, at[v]);
+        else if (p.gate_q) a.y[v] = raw_of<W>(q8_load<E, W>(p.gate_q + e0 + e, at[v]));
       }
     }
   };
@@ -121,13 +121,13 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
 #pragma unroll
         for (int i = 0; i < W; ++i) g[v][i] = q8_at<W>(y, i) > 0 ? g[v][i] : 0.f;
       }
-      own_only<TAIL>(at[v], g[v]);
+      own_only<E>(at[v], g[v]);
       if (p.x) Row<T>::widen(a.x[v], xh[v]);
       else q8_widen<W>(bytes_of<W>(a.x[v]), q8_step(a.b[v]), xh[v]);
       const float m = at[v].live ? a.st.x : 0.f;
 #pragma unroll
       for (int i = 0; i < W; ++i) xh[v][i] = (xh[v][i] - m) * a.st.y;
-      own_only<TAIL>(at[v], xh[v]);
+      own_only<E>(at[v], xh[v]);
 #pragma unroll
       for (int i = 0; i < W; ++i) {
         const float h = g[v][i] * w[v][i];
@@ -145,8 +145,8 @@ template <typename T, int L, int NV, bool TAIL> __global__ void __launch_bounds_
         float dx[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) dx[i] = a.st.y * (g[v][i] * w[v][i] - c1 - xh[v][i] * c2);
-        if (p.dres) Row<T>::template store<TAIL>((T*)p.dres + e0 + e, at[v], Row<T>::narrow(g[v]));
-        Row<T>::template store<TAIL>((T*)p.dx + e0 + e, at[v], Row<T>::narrow(dx));
+        if (p.dres) Row<T>::template store<E>((T*)p.dres + e0 + e, at[v], Row<T>::narrow(g[v]));
+        Row<T>::template store<E>((T*)p.dx + e0 + e, at[v], Row<T>::narrow(dx));
       }
     }
     if constexpr (kAhead) a = next;
@@ -236,7 +236,7 @@ template <typename T> int launch_bwd(const BwdArgs& args, float* workspace, hipS
       a.db = workspace + args.C;
       a.step = 2 * args.C;
     }
-    hipLaunchKernelGGL((k_norm_bwd<T, L, NV, decltype(l)::TAIL>), dim3((unsigned)groups), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_norm_bwd<T, L, NV, decltype(l)::E>), dim3((unsigned)groups), dim3(256), 0, st, a);
     SPC_LAUNCH_CHECK();
     if (a.dw == args.dw) return (int)SPCONV_OK;
     hipLaunchKernelGGL(k_norm_sum, dim3((unsigned)ceil_div(2 * a.C, 16)), dim3(1024), 0, st, workspace, groups, a.C, args.dw, args.db);

@@ -52,9 +52,13 @@ template <typename V> struct __attribute__((packed)) AnyAddress { V v; };
 template <typename V> __device__ __forceinline__ V load_any(const void* p) { return reinterpret_cast<const AnyAddress<V>*>(p)->v; }
 template <typename V> __device__ __forceinline__ void store_any(void* p, V v) { reinterpret_cast<AnyAddress<V>*>(p)->v = v; }
 
+// How a kernel takes the end of a row: widths that are multiples of W, others, and less than W.
+enum Ends { kWholeVectors = 0, kOddWidth = 1, kBelowVector = 2 };
+
 // Where a lane's vector of a row of C channels stands.  The vector that ends a row whose width is no multiple of W reaches back over
 // its neighbour's channels (loaded with one access, like any other): its first `lo` elements are not its own and count as zero.
-// In rows of fewer than W channels `col` is negative and elements are taken one by one.
+// In rows of fewer than W channels `col` is negative and elements are taken one by one (kernels of their own: the addresses of single
+// elements cost the others 64 registers, 170k rows of 450 fp16 179 us for their gradients).
 struct Place {
   int col;    // channel of element 0
   int lo;     // own elements are [lo, W)
@@ -70,16 +74,16 @@ template <typename T> struct Row {
   static constexpr int W = 16 / sizeof(T);
   typedef T vec __attribute__((ext_vector_type(W)));
 
-  // p: element 0 of the vector.  TAIL: widths that are no multiple of W.
-  template <bool TAIL> static __device__ __forceinline__ raw16 load(const T* p, const Place& at, int C) {
-    if (!TAIL || C >= W) return load_any<raw16>(p);
+  // p: element 0 of the vector
+  template <Ends E> static __device__ __forceinline__ raw16 load(const T* p, const Place& at) {
+    if constexpr (E != kBelowVector) return load_any<raw16>(p);
     vec x;
 #pragma unroll
     for (int i = 0; i < W; ++i) x[i] = p[max(i, at.lo)];
     return __builtin_bit_cast(raw16, x);
   }
-  template <bool TAIL> static __device__ __forceinline__ void store(T* p, const Place& at, raw16 r) {
-    if (!TAIL || at.lo == 0) {
+  template <Ends E> static __device__ __forceinline__ void store(T* p, const Place& at, raw16 r) {
+    if (E == kWholeVectors || at.lo == 0) {
       store_any(p, r);
       return;
     }
@@ -101,14 +105,14 @@ template <typename T> struct Row {
   }
 };
 // what stands in front of a vector's own elements becomes zero
-template <bool TAIL, int W> __device__ __forceinline__ void own_only(const Place& at, float (&v)[W]) {
-  if constexpr (TAIL) {
+template <Ends E, int W> __device__ __forceinline__ void own_only(const Place& at, float (&v)[W]) {
+  if constexpr (E != kWholeVectors) {
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = i >= at.lo ? v[i] : 0.f;
   }
 }
-template <bool TAIL, int W> __device__ __forceinline__ void load_floats(const float* p, const Place& at, int C, float (&v)[W]) {
-  if (!TAIL || C >= W) {
+template <Ends E, int W> __device__ __forceinline__ void load_floats(const float* p, const Place& at, float (&v)[W]) {
+  if constexpr (E != kBelowVector) {
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
       const float4x r = load_any<float4x>(p + i);
@@ -142,17 +146,17 @@ template <int W> struct Bytes;  // the q of a vector
 template <> struct Bytes<8> { typedef raw8 word; };
 template <> struct Bytes<4> { typedef unsigned word __attribute__((ext_vector_type(1))); };
 
-template <bool TAIL, int W>
-__device__ __forceinline__ typename Bytes<W>::word q8_load(const signed char* p, const Place& at, int C) {
+template <Ends E, int W>
+__device__ __forceinline__ typename Bytes<W>::word q8_load(const signed char* p, const Place& at) {
   typedef typename Bytes<W>::word word;
-  if (!TAIL || C >= W) return load_any<word>(p);
+  if constexpr (E != kBelowVector) return load_any<word>(p);
   word w = {};
 #pragma unroll
   for (int i = 0; i < W; ++i) w[i / 4] |= (unsigned)(unsigned char)p[max(i, at.lo)] << (8 * (i % 4));
   return w;
 }
-template <bool TAIL, int W> __device__ __forceinline__ void q8_store(signed char* p, const Place& at, typename Bytes<W>::word w) {
-  if (!TAIL || at.lo == 0) {
+template <Ends E, int W> __device__ __forceinline__ void q8_store(signed char* p, const Place& at, typename Bytes<W>::word w) {
+  if (E == kWholeVectors || at.lo == 0) {
     store_any(p, w);
     return;
   }
@@ -204,41 +208,42 @@ template <int G, int W> __device__ __forceinline__ typename Bytes<W>::word q8_qu
 }
 
 // A group of L lanes (32 / W of them, or all, make a block) writes a vector each of the row at q and b.
-template <bool TAIL, int L, int W>
+template <Ends E, int L, int W>
 __device__ __forceinline__ void q8_keep(signed char* q, unsigned char* b, const Place& at, bool live, const float (&v)[W]) {
   constexpr int G = L < kQ8Block / W ? L : kQ8Block / W;
-  unsigned e;
-  const auto w = q8_quantise<G, W>(v, e);
+  unsigned exponent;
+  const auto w = q8_quantise<G, W>(v, exponent);
   if (live) {
-    q8_store<TAIL, W>(q + at.col, at, w);
-    if (threadIdx.x % G == 0) b[at.block] = (unsigned char)e;
+    q8_store<E, W>(q + at.col, at, w);
+    if (threadIdx.x % G == 0) b[at.block] = (unsigned char)exponent;
   }
 }
 
 // Lanes of a row and vectors of a lane: as few lanes as hold the row with one vector each, up to a workgroup's 256, then more
 // vectors (all of a row's lanes in one wave, with 8 vectors or more each, did not fit the registers).  C is 1 to 4096.  Calls go with them as constants.
-template <int LANES, int VECTORS, bool TAIL_> struct Lanes {
+template <int LANES, int VECTORS, Ends ENDS> struct Lanes {
   static constexpr int L = LANES, NV = VECTORS;
-  static constexpr bool TAIL = TAIL_;
+  static constexpr Ends E = ENDS;
 };
 template <int W, typename F> int with_lanes(int C, F go) {
   const int n = (C + W - 1) / W;
+  if (C < W) return go(Lanes<4, 1, kBelowVector>{});
   if (C % W == 0) {
-    if (n <= 4) return go(Lanes<4, 1, false>{});
-    if (n <= 8) return go(Lanes<8, 1, false>{});
-    if (n <= 16) return go(Lanes<16, 1, false>{});
-    if (n <= 32) return go(Lanes<32, 1, false>{});
-    if (n <= 64) return go(Lanes<64, 1, false>{});
+    if (n <= 4) return go(Lanes<4, 1, kWholeVectors>{});
+    if (n <= 8) return go(Lanes<8, 1, kWholeVectors>{});
+    if (n <= 16) return go(Lanes<16, 1, kWholeVectors>{});
+    if (n <= 32) return go(Lanes<32, 1, kWholeVectors>{});
+    if (n <= 64) return go(Lanes<64, 1, kWholeVectors>{});
   }
-  if (n <= 4) return go(Lanes<4, 1, true>{});
-  if (n <= 8) return go(Lanes<8, 1, true>{});
-  if (n <= 16) return go(Lanes<16, 1, true>{});
-  if (n <= 32) return go(Lanes<32, 1, true>{});
-  if (n <= 64) return go(Lanes<64, 1, true>{});
-  if (n <= 128) return go(Lanes<128, 1, true>{});
-  if (n <= 256) return go(Lanes<256, 1, true>{});
-  if (n <= 512) return go(Lanes<256, 2, true>{});
-  if constexpr (W == 4) return go(Lanes<256, 4, true>{});
+  if (n <= 4) return go(Lanes<4, 1, kOddWidth>{});
+  if (n <= 8) return go(Lanes<8, 1, kOddWidth>{});
+  if (n <= 16) return go(Lanes<16, 1, kOddWidth>{});
+  if (n <= 32) return go(Lanes<32, 1, kOddWidth>{});
+  if (n <= 64) return go(Lanes<64, 1, kOddWidth>{});
+  if (n <= 128) return go(Lanes<128, 1, kOddWidth>{});
+  if (n <= 256) return go(Lanes<256, 1, kOddWidth>{});
+  if (n <= 512) return go(Lanes<256, 2, kOddWidth>{});
+  if constexpr (W == 4) return go(Lanes<256, 4, kOddWidth>{});
   return SPCONV_EINVAL;
 }
 
