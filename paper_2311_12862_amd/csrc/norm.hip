@@ -26,7 +26,15 @@ struct FwdArgs {
   float eps;
 };
 
-template <typename T, int L, int NV, Ends E> __global__ void __launch_bounds__(256) k_norm_fwd(const FwdArgs p) {
+// Workgroups a CU holds of a kernel for rows of odd widths: their masks of lanes take scalar registers, of which a wave of eight may
+// have 80 and a wave of seven 96.  Left to themselves these kernels took 90 to 106 and ran as six or seven (80M elements, with no
+// checkpoint, of x and of x and y, us: fp16 450 wide 108, 133, 167, as seven 76, 102, 137, as eight 74, 104, 141; 1000 wide as seven
+// 73, 95, 123, as eight 90, 110, 135; fp32 512 wide 85, 89, 103, as eight 62, 72, 85).  The other kernels take 69 scalar registers and
+// are only slowed by a bound (fp16 448 wide, as eight: 70, 89, 113 -> 79, 108, 139).
+template <typename T, int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E == kOddWidth ? (sizeof(T) == 4 ? 8 : 7) : 0;
+
+template <typename T, int L, int NV, Ends E>
+__global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> : 1)) k_norm_fwd(const FwdArgs p) {
   constexpr int W = Row<T>::W, R = 256 / L;
   __shared__ float part[2][4];
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
@@ -114,9 +122,13 @@ template <typename T, int L, int NV, Ends E> __global__ void __launch_bounds__(2
 template <typename T> int launch_fwd(const FwdArgs& a, hipStream_t st) {
   return with_lanes<Row<T>::W>(a.C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    // as many workgroups as the GPU holds (300k rows of 256 bf16: 85 us, with one workgroup per 256 / L rows 93)
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.rows, 256 / L), 2048);
-    hipLaunchKernelGGL((k_norm_fwd<T, L, NV, decltype(l)::E>), dim3(grid), dim3(256), 0, st, a);
+    constexpr int kHeld = kFwdHeld<T, NV, decltype(l)::E>;
+    const auto kernel = k_norm_fwd<T, L, NV, decltype(l)::E>;
+    static std::atomic<int> held{0};
+    // (one workgroup per 256 / L rows: 300k rows of 256 bf16 with a residual 93 us, so 85)
+    const int groups = kHeld ? 256 * kHeld : resident_groups(kernel, held);
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.rows, 256 / L), groups);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
     SPC_LAUNCH_CHECK();
     return (int)SPCONV_OK;
   });

@@ -213,7 +213,9 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float* __restrict__ par
   }
 }
 
-constexpr int kBwdGroups = 1024;  // workgroups at most: four a CU, as registers allow (300k rows: 512 157 us, 1024 113, 2048 124)
+// Workgroups at most, each with its row of partial sums: five a CU, and no more than the GPU holds (16 bit four, fp32 five to seven).  300k
+// rows of 256 bf16: 512 157 us, 1024 113, 2048 124; 40M fp32 from checkpoints, 448 wide 1024 100, 1280 88, 45 wide 103 and 93.
+constexpr int kBwdGroups = 1280;
 
 // One workgroup for so few elements (counted with the idle lanes) that a second launch - 4 us on the host with its workspace, 4 to 5 on the
 // GPU - costs more than the wait for one row after the other, up to 16 turns of 0.5 to 0.9 us; it writes dw and db itself.  A call, us, one
@@ -229,14 +231,18 @@ bool alone(int64_t rows, int C) {
 template <typename T> int launch_bwd(const BwdArgs& args, float* workspace, hipStream_t st) {
   return with_lanes<Row<T>::W>(args.C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    const int groups = alone(args.rows, args.C) ? 1 : (int)std::min<int64_t>(ceil_div(args.rows, 256 / L), kBwdGroups);
+    const auto kernel = k_norm_bwd<T, L, NV, decltype(l)::E>;
+    static std::atomic<int> held{0};
+    const int groups = alone(args.rows, args.C)
+                           ? 1
+                           : (int)std::min<int64_t>(ceil_div(args.rows, 256 / L), std::min(kBwdGroups, resident_groups(kernel, held)));
     BwdArgs a = args;
     if (args.dw && !alone(args.rows, args.C)) {
       a.dw = workspace;
       a.db = workspace + args.C;
       a.step = 2 * args.C;
     }
-    hipLaunchKernelGGL((k_norm_bwd<T, L, NV, decltype(l)::E>), dim3((unsigned)groups), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
     SPC_LAUNCH_CHECK();
     if (a.dw == args.dw) return (int)SPCONV_OK;
     hipLaunchKernelGGL(k_norm_sum, dim3((unsigned)ceil_div(2 * a.C, 16)), dim3(1024), 0, st, workspace, groups, a.C, args.dw, args.db);

@@ -3,6 +3,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 namespace spc {
 namespace {
 
@@ -217,6 +219,23 @@ __device__ __forceinline__ void q8_keep(signed char* q, unsigned char* b, const 
     q8_store<E, W>(q + at.col, at, w);
     if (threadIdx.x % G == 0) b[at.block] = (unsigned char)exponent;
   }
+}
+
+// Workgroups of a kernel that the GPU holds at once: a kernel that loops over rows is launched with no more, or the ones that wait run as
+// a second round after the others (fp16 forward with 66 registers, seven workgroups a CU, launched with eight: 300k x 256 88 us, with
+// seven 64).  `held` caches the answer, one for each kernel.
+template <typename K> int resident_groups(K kernel, std::atomic<int>& held) {
+  int n = held.load(std::memory_order_relaxed);
+  if (n == 0) {
+    int per_cu = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, 256, 0) != hipSuccess || per_cu < 1) {
+      (void)hipGetLastError();
+      per_cu = 4;
+    }
+    n = 256 * per_cu;
+    held.store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 // Lanes of a row and vectors of a lane: as few lanes as hold the row with one vector each, up to a workgroup's 256, then more
