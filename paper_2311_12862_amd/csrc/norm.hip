@@ -27,10 +27,10 @@ struct FwdArgs {
 };
 
 // Workgroups a CU holds of a kernel for rows of odd widths: their masks of lanes take scalar registers, of which a wave of eight may
-// have 80 and a wave of seven 96.  Left to themselves these kernels took 90 to 106 and ran as six or seven (80M elements, with no
-// checkpoint, of x and of x and y, us: fp16 450 wide 108, 133, 167, as seven 76, 102, 137, as eight 74, 104, 141; 1000 wide as seven
-// 73, 95, 123, as eight 90, 110, 135; fp32 512 wide 85, 89, 103, as eight 62, 72, 85).  The other kernels take 69 scalar registers and
-// are only slowed by a bound (fp16 448 wide, as eight: 70, 89, 113 -> 79, 108, 139).
+// have 80 and a wave of seven 96, and which the count of resident workgroups leaves out.  With 90 to 106 they ran as six or seven after
+// launches of seven or eight (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us: fp16 450 wide 108, 133, 167,
+// now 75, 96, 128; as eight 74, 104, 141; fp32 512 wide 85, 89, 103, as eight 61, 69, 82).  The other kernels take 69, and a bound
+// slows them (fp16 448 wide as eight: 70, 89, 113 -> 79, 108, 139).
 template <typename T, int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E == kOddWidth ? (sizeof(T) == 4 ? 8 : 7) : 0;
 
 template <typename T, int L, int NV, Ends E>

@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float* __restrict__ par
 }
 
 // Workgroups at most, each with its row of partial sums: five a CU, and no more than the GPU holds (16 bit four, fp32 five to seven).  300k
-// rows of 256 bf16: 512 157 us, 1024 113, 2048 124; 40M fp32 from checkpoints, 448 wide 1024 100, 1280 88, 45 wide 103 and 93.
+// rows of 256 bf16: 512 157 us, 1024 113, 2048 124; 38M elements in fp32 from checkpoints, 448 wide 1024 100, 1280 88, 45 wide 103 and 93.
 constexpr int kBwdGroups = 1280;
 
 // One workgroup for so few elements (counted with the idle lanes) that a second launch - 4 us on the host with its workspace, 4 to 5 on the

@@ -54,6 +54,26 @@ template <typename V> struct __attribute__((packed)) AnyAddress { V v; };
 template <typename V> __device__ __forceinline__ V load_any(const void* p) { return reinterpret_cast<const AnyAddress<V>*>(p)->v; }
 template <typename V> __device__ __forceinline__ void store_any(void* p, V v) { reinterpret_cast<AnyAddress<V>*>(p)->v = v; }
 
+// The last n bytes of N words whose first stands at p, 1 to 4 N - S of them, a multiple of S: the last eight if n has that bit, in
+// front of them four, two and one.  Every piece is the end of one of the words, so nothing is shifted by a lane's own number.  (One
+// element after the other, with a mask of lanes for each: 1.7M rows of 45 fp16 forward 139 us, so 106, gradients 160, so 120.)
+template <int S, typename V> __device__ __forceinline__ void store_end(char* p, int n, V w) {
+  constexpr int N = sizeof(V) / 4;
+  asm volatile("" : "+v"(n));  // (conditions and addresses that hold for every row would be kept in registers all along)
+  if constexpr (N == 4)
+    if (n & 8) store_any(p + 8, raw8{w[2], w[3]});
+  if constexpr (N > 1)
+    if (n & 4) store_any(p + (4 * N - (n & ~3)), N == 4 && (n & 8) ? w[1] : w[N - 1]);
+  if constexpr (S < 4) {
+    unsigned front = w[N - 1];  // the word that the rest ends
+#pragma unroll
+    for (int j = 1; j < N; ++j) front = n >> 2 == j ? w[N - 1 - j] : front;
+    if (n & 2) store_any(p + (4 * N - (n & ~1)), (unsigned short)(front >> 16));
+    if constexpr (S == 1)
+      if (n & 1) p[4 * N - n] = (char)(n & 2 ? front >> 8 : front >> 24);
+  }
+}
+
 // How a kernel takes the end of a row: widths that are multiples of W, others, and less than W.
 enum Ends { kWholeVectors = 0, kOddWidth = 1, kBelowVector = 2 };
 
@@ -85,14 +105,8 @@ template <typename T> struct Row {
     return __builtin_bit_cast(raw16, x);
   }
   template <Ends E> static __device__ __forceinline__ void store(T* p, const Place& at, raw16 r) {
-    if (E == kWholeVectors || at.lo == 0) {
-      store_any(p, r);
-      return;
-    }
-    const vec x = __builtin_bit_cast(vec, r);
-#pragma unroll
-    for (int i = 1; i < W; ++i)
-      if (i >= at.lo) p[i] = x[i];
+    if (E == kWholeVectors || at.lo == 0) store_any(p, r);
+    else store_end<sizeof(T)>((char*)p, (W - at.lo) * (int)sizeof(T), r);
   }
   static __device__ __forceinline__ void widen(raw16 r, float (&v)[W]) {
     const vec x = __builtin_bit_cast(vec, r);
@@ -158,13 +172,8 @@ __device__ __forceinline__ typename Bytes<W>::word q8_load(const signed char* p,
   return w;
 }
 template <Ends E, int W> __device__ __forceinline__ void q8_store(signed char* p, const Place& at, typename Bytes<W>::word w) {
-  if (E == kWholeVectors || at.lo == 0) {
-    store_any(p, w);
-    return;
-  }
-#pragma unroll
-  for (int i = 1; i < W; ++i)
-    if (i >= at.lo) p[i] = (signed char)(w[i / 4] >> (8 * (i % 4)));
+  if (E == kWholeVectors || at.lo == 0) store_any(p, w);
+  else store_end<1>((char*)p, W - at.lo, w);
 }
 template <int W> __device__ __forceinline__ int q8_at(typename Bytes<W>::word w, int i) { return (signed char)(w[i / 4] >> (8 * (i % 4))); }
 template <int W> __device__ __forceinline__ void q8_widen(typename Bytes<W>::word w, float step, float (&v)[W]) {
