@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(256) k_q8_pack(const T* __restrict__ x, Q8Ref 
       float f[W];
       Row<T>::widen(raw, f);
       own_only<E>(at, f);
-      q8_keep<E, L, W>(q + rl * C, b + rl * nb, at, live, f);
+      q8_keep<E, L, W>(q + (rl * C + at.col), b + (rl * nb + at.block), at, live, f);
     }
   }
 }

@@ -4,7 +4,7 @@
 //
 // A group of L lanes holds one row in registers, so every tensor crosses the memory once; statistics are taken in two passes
 // over the registers, in fp32.  Memory bounds it: 300k rows of 256 bf16 with a residual 85 us, 5.4 TB/s; 100k rows of 64 f16 with
-// both checkpoints 11.9 us (12.2 before 8-bit rounding took 9 instructions an element).
+// both checkpoints 11.9 us; 300k of 256 f16 with both 98 (103 where 8-bit rounding took 9 instructions an element), 4.8 TB/s.
 #include "common.h"
 #include "rows.h"
 
@@ -26,24 +26,27 @@ struct FwdArgs {
   float eps;
 };
 
-// Workgroups a CU holds of a kernel for rows of odd widths: their masks of lanes take scalar registers, of which a wave of eight may
-// have 80 and a wave of seven 96, and which the count of resident workgroups leaves out.  With 90 to 106 they ran as six or seven after
-// launches of seven or eight (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us: fp16 450 wide 108, 133, 167,
-// now 75, 96, 128; as eight 74, 104, 141; fp32 512 wide 85, 89, 103, as eight 61, 69, 82).  The other kernels take 69, and a bound
-// slows them (fp16 448 wide as eight: 70, 89, 113 -> 79, 108, 139).
-template <typename T, int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E == kOddWidth ? (sizeof(T) == 4 ? 8 : 7) : 0;
+// Workgroups a CU is to hold where a lane has one vector.  Scalar registers decide it (masks of lanes, bases of nine tensors): a wave of
+// eight has 80 of them, which the count of resident workgroups leaves out.  For want of 2 to 30 of them launches of eight ran as seven or
+// six, with a second round (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us: fp32 256 wide 81, 102, 110,
+// bounded 58, 73, 83; fp16 450 wide 108, 133, 167, bounded 72, 95, 128; fp32 512 wide 85, 89, 103, bounded 62, 70, 83).
+template <int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E != kBelowVector ? 8 : 0;
 
 template <typename T, int L, int NV, Ends E>
-__global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> : 1)) k_norm_fwd(const FwdArgs p) {
+__global__ void __launch_bounds__(256, (kFwdHeld<NV, E> ? kFwdHeld<NV, E> : 1)) k_norm_fwd(const FwdArgs p) {
   constexpr int W = Row<T>::W, R = 256 / L;
   __shared__ float part[2][4];
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
   const int C = p.C;
   const float inv = 1.f / (float)C;
   Place at[NV];
+  int element[NV], block[NV];  // behind the workgroup's first row, which all its lanes share
 #pragma unroll
-  for (int v = 0; v < NV; ++v) at[v] = place_in_row<W>(v * L + lane, C);
-  // (the workgroup's first row is the same for all its lanes: addresses are a scalar base and 32 bits per lane)
+  for (int v = 0; v < NV; ++v) {
+    at[v] = place_in_row<W>(v * L + lane, C);
+    element[v] = rl * C + at[v].col;
+    block[v] = rl * p.nb + at[v].block;
+  }
   for (long long r0 = (long long)blockIdx.x * R; r0 < p.rows; r0 += (long long)gridDim.x * R) {
     const bool row = rl < p.rows - r0;
     const long long e0 = r0 * C;
@@ -52,11 +55,13 @@ __global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> 
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      each_row(element[v]);
+      each_row(block[v]);
+      each_row(at[v].col);
       raw[v] = res[v] = raw16{0, 0, 0, 0};
       if (row && at[v].live) {
-        const int e = rl * C + at[v].col;
-        raw[v] = Row<T>::template load<E>((const T*)p.x + e0 + e, at[v]);
-        if (p.res) res[v] = Row<T>::template load<E>((const T*)p.res + e0 + e, at[v]);
+        raw[v] = Row<T>::template load<E>(behind<E>((const T*)p.x + e0, element[v]), at[v]);
+        if (p.res) res[v] = Row<T>::template load<E>(behind<E>((const T*)p.res + e0, element[v]), at[v]);
       }
     }
 #pragma unroll
@@ -64,7 +69,7 @@ __global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> 
       Row<T>::widen(raw[v], x[v]);
       own_only<E>(at[v], x[v]);
       if (p.kept_x.q)
-        q8_keep<E, L, W>(p.kept_x.q + e0 + rl * C, p.kept_x.b + r0 * p.nb + rl * p.nb, at[v], row && at[v].live, x[v]);
+        q8_keep<E, L, W>(behind<E>(p.kept_x.q + e0, element[v]), behind<E>(p.kept_x.b + r0 * p.nb, block[v]), at[v], row && at[v].live, x[v]);
 #pragma unroll
       for (int i = 0; i < W; ++i) sum += x[v][i];
     }
@@ -89,12 +94,12 @@ __global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> 
 #pragma unroll
       for (int i = 0; i < W; ++i) y[i] = x[v][i] * rstd;
       if (p.w) {
-        if (live) load_floats<E, W>(p.w + at[v].col, at[v], t);
+        if (live) load_floats<E, W>(behind<E>(p.w, at[v].col), at[v], t);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] *= t[i];
       }
       if (p.b) {
-        if (live) load_floats<E, W>(p.b + at[v].col, at[v], t);
+        if (live) load_floats<E, W>(behind<E>(p.b, at[v].col), at[v], t);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] += t[i];
       }
@@ -108,12 +113,12 @@ __global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> 
         for (int i = 0; i < W; ++i) y[i] = __builtin_elementwise_maximum(y[i], 0.f);  // (a NaN stays one)
       }
       const raw16 out = Row<T>::narrow(y);
-      if (live) Row<T>::template store<E>((T*)p.y + e0 + (rl * C + at[v].col), at[v], out);
+      if (live) Row<T>::template store<E>(behind<E>((T*)p.y + e0, element[v]), at[v], out);
       if (p.kept_y.q) {  // of what was written
         Row<T>::widen(out, y);
 #pragma unroll
         for (int i = 0; i < W; ++i) y[i] = live && (E == kWholeVectors || i >= at[v].lo) ? y[i] : 0.f;
-        q8_keep<E, L, W>(p.kept_y.q + e0 + rl * C, p.kept_y.b + r0 * p.nb + rl * p.nb, at[v], live, y);
+        q8_keep<E, L, W>(behind<E>(p.kept_y.q + e0, element[v]), behind<E>(p.kept_y.b + r0 * p.nb, block[v]), at[v], live, y);
       }
     }
   }
@@ -122,7 +127,7 @@ __global__ void __launch_bounds__(256, (kFwdHeld<T, NV, E> ? kFwdHeld<T, NV, E> 
 template <typename T> int launch_fwd(const FwdArgs& a, hipStream_t st) {
   return with_lanes<Row<T>::W>(a.C, [&](auto l) {
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
-    constexpr int kHeld = kFwdHeld<T, NV, decltype(l)::E>;
+    constexpr int kHeld = kFwdHeld<NV, decltype(l)::E>;
     const auto kernel = k_norm_fwd<T, L, NV, decltype(l)::E>;
     static std::atomic<int> held{0};
     // (one workgroup per 256 / L rows: 300k rows of 256 bf16 with a residual 93 us, so 85)

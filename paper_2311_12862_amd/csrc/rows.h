@@ -3,7 +3,9 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 namespace spc {
 namespace {
@@ -91,6 +93,16 @@ template <int W> __device__ __forceinline__ Place place_in_row(int vector, int C
   const int first = vector * W, n = C - first;
   return {n >= W ? first : C - W, n >= W ? 0 : W - n, first / 32, n > 0};
 }
+
+// Element i behind a base that all lanes of a wave share: 32 bits a lane.  (In rows of fewer than W channels a vector starts in front of
+// its row, i may be negative.)
+template <Ends E, typename T> __device__ __forceinline__ T* behind(T* base, int i) {
+  typedef std::conditional_t<std::is_const_v<T>, const char, char> byte;
+  if constexpr (E == kBelowVector) return base + i;
+  else return (T*)((byte*)base + (unsigned)(i * (int)sizeof(T)));
+}
+// Keeps the compiler from computing what follows from v for all rows at once and holding it: addresses of 64 bits for every tensor.
+__device__ __forceinline__ void each_row(int& v) { asm volatile("" : "+v"(v)); }
 
 template <typename T> struct Row {
   static constexpr int W = 16 / sizeof(T);
@@ -183,12 +195,13 @@ template <int W> __device__ __forceinline__ void q8_widen(typename Bytes<W>::wor
 
 // The checkpoint of a vector, one of the G that make a block (aligned groups of G lanes; every lane of the group takes part, with zeros
 // where it has no elements).  What bounds a kernel that keeps two checkpoints is the vector unit as soon as an element takes more
-// than about 50 instructions; this takes 9.  Rounding is that of an addition: 1.5 * 2^23 + r has r to nearest even in its
+// than about 50 instructions; this takes 6.  Rounding is that of an addition: 1.5 * 2^23 + r has r to nearest even in its
 // low bits.
 template <int G, int W> __device__ __forceinline__ typename Bytes<W>::word q8_quantise(const float (&v)[W], unsigned& b) {
-  unsigned top = 0;
+  float most = __builtin_fabsf(v[0]);
 #pragma unroll
-  for (int i = 0; i < W; ++i) top = max(top, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
+  for (int i = 1; i < W; ++i) most = __builtin_elementwise_maximum(most, __builtin_fabsf(v[i]));  // (a NaN stays one)
+  unsigned top = __builtin_bit_cast(unsigned, most) & 0x7FFFFFFFu;
   top = group_max<G>(top);
   b = max(top >> 23, 1u);
   // 2^(133 - b) is a number from b = 6 on; below (magnitudes under 2^-121) v_ldexp scales.  Products are exact, except for values so
@@ -204,9 +217,9 @@ template <int G, int W> __device__ __forceinline__ typename Bytes<W>::word q8_qu
   unsigned s[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    // (at most 127: 128 would be the rounding of values from 127.5 on; at least 1, by 0.75, where the value is not 0)
-    const float m = __builtin_amdgcn_fmed3f(__builtin_fabsf(t[i]), 0.75f, 127.f);
-    const float r = v[i] != 0.f ? __builtin_copysignf(m, v[i]) : 0.f;
+    // (at most 127: 128 would be the rounding of values from 127.5 on; at least 1 where the value is not 0, whatever its size)
+    const float least = __builtin_amdgcn_fmed3f(ldexpf(__builtin_fabsf(v[i]), 150), 0.f, 1.f);
+    const float r = __builtin_copysignf(__builtin_amdgcn_fmed3f(__builtin_fabsf(t[i]), least, 127.f), v[i]);
     s[i] = __builtin_bit_cast(unsigned, r + 12582912.f);
   }
   typename Bytes<W>::word w;
@@ -218,21 +231,22 @@ template <int G, int W> __device__ __forceinline__ typename Bytes<W>::word q8_qu
   return w;
 }
 
-// A group of L lanes (32 / W of them, or all, make a block) writes a vector each of the row at q and b.
+// A group of L lanes (32 / W of them, or all, make a block) writes a vector each, its element 0 at q, its block at b.
 template <Ends E, int L, int W>
 __device__ __forceinline__ void q8_keep(signed char* q, unsigned char* b, const Place& at, bool live, const float (&v)[W]) {
   constexpr int G = L < kQ8Block / W ? L : kQ8Block / W;
   unsigned exponent;
   const auto w = q8_quantise<G, W>(v, exponent);
   if (live) {
-    q8_store<E, W>(q + at.col, at, w);
-    if (threadIdx.x % G == 0) b[at.block] = (unsigned char)exponent;
+    q8_store<E, W>(q, at, w);
+    if (threadIdx.x % G == 0) *b = (unsigned char)exponent;
   }
 }
 
 // Workgroups of a kernel that the GPU holds at once: a kernel that loops over rows is launched with no more, or the ones that wait run as
-// a second round after the others (fp16 forward with 66 registers, seven workgroups a CU, launched with eight: 300k x 256 88 us, with
-// seven 64).  `held` caches the answer, one for each kernel.
+// a second round after the others (fp16 forward with seven a CU, launched with eight: 300k x 256 88 us, with seven 64).  At most six a
+// CU: the count leaves out scalar registers, and six is what is held of kernels that take all of them.  `held` caches the answer, one for
+// each kernel.
 template <typename K> int resident_groups(K kernel, std::atomic<int>& held) {
   int n = held.load(std::memory_order_relaxed);
   if (n == 0) {
@@ -241,7 +255,7 @@ template <typename K> int resident_groups(K kernel, std::atomic<int>& held) {
       (void)hipGetLastError();
       per_cu = 4;
     }
-    n = 256 * per_cu;
+    n = 256 * std::min(per_cu, 6);
     held.store(n, std::memory_order_relaxed);
   }
   return n;
