@@ -213,9 +213,12 @@ __global__ void __launch_bounds__(1024) k_norm_sum(const float* __restrict__ par
   }
 }
 
-// Workgroups at most, each with its row of partial sums: five a CU, and no more than the GPU holds (16 bit four, fp32 five to seven).  300k
-// rows of 256 bf16: 512 157 us, 1024 113, 2048 124; 38M elements in fp32 from checkpoints, 448 wide 1024 100, 1280 88, 45 wide 103 and 93.
+// Workgroups at most, each with its row of partial sums, and no more than the GPU holds: four a CU (300k rows of 256 bf16: 512 157 us, 1024
+// 113, 2048 124); five where x is a checkpoint, with fewer bytes to wait for and more to compute, and a workgroup has 16 turns or more, so
+// that the longer sum is made up for.  1024 and 1280, us: from checkpoints 300k x 256 fp16 96 and 94, 170k x 448 101 and 96, x 450 fp32 191 and
+// 169, 40k x 256 fp16 20.0 and 21.6, 100k x 64 15.6 and 17.4; from tensors 300k x 256 92 and 95, 170k x 450 fp32 173 and 184.
 constexpr int kBwdGroups = 1280;
+int bwd_groups(bool kept, int64_t blocks) { return kept && blocks >= 16 * kBwdGroups ? kBwdGroups : 1024; }
 
 // One workgroup for so few elements (counted with the idle lanes) that a second launch - 4 us on the host with its workspace, 4 to 5 on the
 // GPU - costs more than the wait for one row after the other, up to 16 turns of 0.5 to 0.9 us; it writes dw and db itself.  A call, us, one
@@ -233,9 +236,10 @@ template <typename T> int launch_bwd(const BwdArgs& args, float* workspace, hipS
     constexpr int L = decltype(l)::L, NV = decltype(l)::NV;
     const auto kernel = k_norm_bwd<T, L, NV, decltype(l)::E>;
     static std::atomic<int> held{0};
+    const int64_t blocks = ceil_div(args.rows, 256 / L);
     const int groups = alone(args.rows, args.C)
                            ? 1
-                           : (int)std::min<int64_t>(ceil_div(args.rows, 256 / L), std::min(kBwdGroups, resident_groups(kernel, held)));
+                           : (int)std::min<int64_t>(blocks, std::min(bwd_groups(!args.x, blocks), resident_groups(kernel, held)));
     BwdArgs a = args;
     if (args.dw && !alone(args.rows, args.C)) {
       a.dw = workspace;
