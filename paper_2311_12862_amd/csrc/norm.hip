@@ -4,7 +4,7 @@
 //
 // A group of L lanes holds one row in registers, so every tensor crosses the memory once; statistics are taken in two passes
 // over the registers, in fp32.  Memory bounds it: 300k rows of 256 bf16 with a residual 85 us, 5.4 TB/s; 100k rows of 64 f16 with
-// both checkpoints 11.9 us; 300k of 256 f16 with both 98 (103 where 8-bit rounding took 9 instructions an element), 4.8 TB/s.
+// both checkpoints 10.9 us; 300k of 256 f16 with both 98 (103 where 8-bit rounding took 9 instructions an element), 4.8 TB/s.
 #include "common.h"
 #include "rows.h"
 
