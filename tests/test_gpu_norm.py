@@ -363,3 +363,13 @@ def test_eps_of_zero_and_a_large_one():
     assert (dx == 0).all() and (dw == 0).all() and (db == 0).all()
     y, _ = sp.layer_norm_fwd(x, w, b, 1e30)
     assert (y - b).abs().max().item() < 1e-12 + 2 ** -24 * b.abs().max().item()
+
+
+@pytest.mark.parametrize("dtype", DTS)
+@pytest.mark.parametrize("first", [9, 33, 129, 521])
+def test_every_end_of_a_row(dtype, first):
+    """Widths that leave 0 to 7 elements behind the last whole vector, rows at odd addresses, in a group of lanes of each kind."""
+    for c in range(first, first + 8):
+        for rows in (1, 67):
+            _check_fwd(rows, c, dtype, True, True, True, shift=c % 3)
+            _check_bwd(rows, c, dtype, True, True, True, 2 * (c % 2), shift=c % 3)
