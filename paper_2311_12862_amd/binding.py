@@ -7,6 +7,8 @@ Stream ordering: every call enqueues its work on `stream` (default: torch's
 current stream) and returns without waiting.  A tensor that a call returns or
 fills is therefore ordered on that stream only: read it on the same stream, or
 synchronise that stream first (`tensor.cpu()` runs on torch's current stream).
+Layer norm and the calls on checkpoints take their results' memory and their
+workspaces from torch's pool of the stream that they run on.
 """
 from __future__ import annotations
 
@@ -394,23 +396,22 @@ def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=N
     return out
 
 
-def _wgrad_q8(kept, dout, kmap, cfg, out, stream):
+def _wgrad_q8(kept, dout, kmap, cfg, out, stream=None):
     dt, shape, dev = _row_args(dout)
     if shape[0] != kmap.n_out or kept.rows != kmap.n_in:
         raise SpconvError(-5, f"rows of the checkpoint ({kept.rows}) or of dout {tuple(shape)} do not fit the kmap "
                               f"({kmap.n_in} in, {kmap.n_out} out)")
     if kept.get_device() != dev:
         raise ValueError(f"tensors on {dout.device} and {kept.device}")
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return _wgrad_q8(kept, dout, kmap, cfg, out, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, _wgrad_q8, kept, dout, kmap, cfg, out)
     c_in, c_out = kept.channels, shape[1]
     if out is None:
         out = dout.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
     else:
         _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, dout)
     status = _LIB.spconv_wgrad_q8(kept.byref, dout.data_ptr() or None, kmap.handle, c_in, c_out, dt, _cfg(cfg), out.data_ptr(),
-                                  _stream_on(stream, dev))
+                                  _stream_here(dev))
     if status:
         _check(status, "spconv_wgrad_q8")
     return out
@@ -477,23 +478,22 @@ def ew(op: int, a, b=None, out=None, stream=None):
     return out
 
 
-def _relu_bwd_q8(op, a, kept, out, stream):
+def _relu_bwd_q8(op, a, kept, out, stream=None):
     if op != EW_RELU_BWD:
         raise ValueError("a Checkpoint stands for the output of EW_RELU_BWD only")
     dt, shape, dev = _row_args(a)
     if shape != (kept.rows, kept.channels):
         raise ValueError("shape mismatch")
     ref = _kept_like(kept, a, shape, dev)
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return _relu_bwd_q8(op, a, kept, out, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, _relu_bwd_q8, op, a, kept, out)
     if out is None:
         out = torch.empty_like(a)
         to = out.data_ptr() or None
     else:
         to = _like(out, a, shape, dev)
     status = (_LIB or load_library()).spconv_relu_bwd_q8(a.data_ptr() or None, ref, to, kept.rows * kept.channels, dt,
-                                                         _stream_on(stream, dev))
+                                                         _stream_here(dev))
     if status:
         _check(status, "spconv_relu_bwd_q8")
     return out
@@ -525,11 +525,31 @@ def _device_now():
     return _device_now()
 
 
-def _stream_on(stream, dev):
-    """_stream for a call whose device is known to be the current one."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(dev)
-    return _stream(stream)
+def _stream_here(dev):
+    """_stream(None) where the current device's number is known."""
+    return _raw_stream(dev) if _raw_stream is not None else _stream(None)
+
+
+def _elsewhere(dev, stream, call, *args):
+    """call(*args) with device dev current, and on it `stream` unless that is None.  What the call allocates then comes from the pool
+    of the stream that uses it: a block of another stream's pool may still be read or written by that one's kernels.  The tensors that it
+    returns may be read on the stream that was current before as well, once the caller has ordered the two; torch is told, so that it
+    keeps a block that is given back until that stream is done with it."""
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {dev}")
+    if dev != _device_now():
+        with torch.cuda.device(dev):
+            return _elsewhere(dev, stream, call, *args)
+    handle = None if stream is None else _stream(stream)
+    if handle is None or handle == _stream_here(dev):
+        return call(*args)
+    before = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)):
+        made = call(*args)
+    for t in made if isinstance(made, tuple) else (made,):
+        if t is not None:
+            t.record_stream(before)
+    return made
 
 
 def _row_args(x):
@@ -625,18 +645,22 @@ class Checkpoint:
     def get_device(self) -> int:
         return self._data.get_device()
 
+    def record_stream(self, stream):
+        self._data.record_stream(stream)
+        if isinstance(self._exps, torch.Tensor):
+            self._exps.record_stream(stream)
+
 
 def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """spconv_q8_pack: the 8-bit checkpoint of x [rows, channels]."""
     dt, shape, dev = _row_args(x)
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return q8_pack(x, out, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, q8_pack, x, out)
     rows, channels = shape
     if out is None:
         out = Checkpoint.empty(rows, channels)
     status = (_LIB or load_library()).spconv_q8_pack(x.data_ptr() or None, rows, channels, dt, _kept_like(out, x, shape, dev),
-                                                     _stream_on(stream, dev))
+                                                     _stream_here(dev))
     if status:
         _check(status, "spconv_q8_pack")
     return out
@@ -648,16 +672,15 @@ def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
     if dt is None:
         raise ValueError(f"unsupported dtype {dtype}")
     dev = kept.get_device()
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return q8_unpack(kept, dtype, out, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, q8_unpack, kept, dtype, out)
     rows, channels = kept.rows, kept.channels
     if out is None:
         out = kept._data.new_empty((rows, channels), dtype=dtype)
     else:
         _out_tensor(out, (rows, channels), dtype, kept)
     status = (_LIB or load_library()).spconv_q8_unpack(kept.byref, rows, channels, dt, out.data_ptr() or None,
-                                                       _stream_on(stream, dev))
+                                                       _stream_here(dev))
     if status:
         _check(status, "spconv_q8_unpack")
     return out
@@ -669,9 +692,8 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     weight and bias fp32 [channels], stats fp32 [rows, 2] = (mean, 1 / std) for layer_norm_bwd.  keep_x and keep_y are
     filled with checkpoints of x and y in the same pass."""
     dt, shape, dev = _row_args(x)
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return layer_norm_fwd(x, weight, bias, eps, relu, residual, out, keep_x, keep_y, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, layer_norm_fwd, x, weight, bias, eps, relu, residual, out, keep_x, keep_y)
     rows, channels = shape
     w = None if weight is None else _floats(weight, (channels,), x, dev)
     b = None if bias is None else _floats(bias, (channels,), x, dev)
@@ -686,7 +708,7 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, relu: bool = Fa
     stats = x.new_empty((rows, 2), dtype=torch.float32)
     status = (_LIB or load_library()).spconv_layer_norm_fwd(
         x.data_ptr() or None, res, w, b, eps, 1 if relu else 0, rows, channels, dt, y, stats.data_ptr() or None, kept_x, kept_y,
-        _stream_on(stream, dev))
+        _stream_here(dev))
     if status:
         _check(status, "spconv_layer_norm_fwd")
     return out, stats
@@ -697,9 +719,8 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
     Checkpoint of it; gate: its output or the Checkpoint of it where it had a ReLU.  dweight and dbias are fp32 [channels]
     (None for affine=False), dresidual is None unless residual is set."""
     dt, shape, dev = _row_args(dout)
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return layer_norm_bwd(dout, x, stats, weight, gate, residual, affine, stream)
+    if stream is not None or dev != _device_now():
+        return _elsewhere(dev, stream, layer_norm_bwd, dout, x, stats, weight, gate, residual, affine)
     rows, channels = shape
     stats_ptr = _floats(stats, (rows, 2), dout, dev)
     w = None if weight is None else _floats(weight, (channels,), dout, dev)
@@ -717,7 +738,7 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
     lib = _LIB or load_library()
     dx = torch.empty_like(dout)
     dres = torch.empty_like(dout) if residual else None
-    dweight = dbias = dw_ptr = db_ptr = workspace = ws_ptr = None
+    dweight = dbias = dw_ptr = db_ptr = ws_ptr = None
     need = 0
     if affine:
         need = lib.spconv_layer_norm_bwd_workspace(rows, channels)
@@ -729,13 +750,9 @@ def layer_norm_bwd(dout, x, stats, weight=None, gate=None, residual: bool = Fals
         if need:
             workspace = stats.new_empty((need // 4,))
             ws_ptr = workspace.data_ptr()
-    st = _stream_on(stream, dev)
     status = lib.spconv_layer_norm_bwd(dout.data_ptr() or None, x_ptr, kept_x, y_ptr, kept_y, w, stats_ptr, rows, channels, dt,
                                        dx.data_ptr() or None, None if dres is None else dres.data_ptr() or None, dw_ptr, db_ptr,
-                                       ws_ptr, need, st)
+                                       ws_ptr, need, _stream_here(dev))
     if status:
         _check(status, "spconv_layer_norm_bwd")
-    if workspace is not None and stream is not None and st != _stream(None):
-        # the caller's stream is still to use it when this function lets go of it
-        workspace.record_stream(torch.cuda.ExternalStream(st, device=dout.device))
     return dx, dweight, dbias, dres
