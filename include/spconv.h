@@ -329,9 +329,11 @@ SPCONV_API int spconv_wgrad(const void* feats, const void* dout, spconv_kmap* km
  *   data  device int8  [rows][C]
  *   exps  device uint8 [rows][ceil(C / 32)]
  * Each row is cut into blocks of 32 channels (the last one shorter).  A block's b in exps is the biased fp32 exponent of its
- * largest magnitude, at least 1; a channel's q in data, -127..127, stands for q * 2^(b - 133), exactly, in every dtype.  q is the
- * value over the step 2^(b - 133), rounded to nearest even, at most 127 in magnitude, and +-1 where a value other than 0 would round
- * to 0.  So a value is off by at most half a step - one step where it is kept from rounding to 128 or to 0 - which is
+ * largest magnitude, at least 1; a channel's q in data, -127..127, stands for q * 2^(b - 133).  That is a number of the tensor's own
+ * dtype, of fp32 and of bf16; read as fp16, a checkpoint of an fp32 or bf16 tensor is rounded to nearest even: to infinity from 65520 on
+ * (in blocks with b >= 143) and to multiples of 2^-24.  (A checkpoint does not know what it was made from; norm gradients take the
+ * value itself, in fp32.)  q is the value over the step 2^(b - 133), rounded to nearest even, at most 127 in magnitude, and +-1 where a
+ * value other than 0 would round to 0.  So a value is off by at most half a step - one step where it is kept from rounding to 128 or to 0 - which is
  * 2^-7 (2^-6) of the block's largest magnitude; its sign is always right.  A block with an infinity or a NaN has b = 255 and
  * q = 0, and stands for NaN throughout (b = 255 does, whatever q is).
  * Both pointers belong to the caller and need no alignment; C is 1 to 4096, rows * C at most 2^40.  Rows with a large offset
@@ -352,8 +354,8 @@ SPCONV_API int spconv_q8_unpack(const spconv_q8* kept, int64_t rows, int C, spco
  * out may be dout. */
 SPCONV_API int spconv_relu_bwd_q8(const void* dout, const spconv_q8* kept, void* out, int64_t n, spconv_dtype dtype, void* stream);
 
-/* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout.  The values are exact in dtype: the result is
- * that of spconv_wgrad on the unpacked tensor.  16-bit layers on kmaps of K < 5 gather data itself where it is 4-byte aligned
+/* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout, and the values are read as dtype: the
+ * result is that of spconv_wgrad on the tensor that spconv_q8_unpack makes.  16-bit layers on kmaps of K < 5 gather data itself where it is 4-byte aligned
  * (narrow ones on dense maps, whose gradient comes from the map, do not); others unpack it first, into memory that the kmap then keeps (one
  * call before a capture makes it). */
 SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,

@@ -155,9 +155,9 @@ template <Ends E, int W> __device__ __forceinline__ void load_floats(const float
 
 // ---- 8-bit checkpoints.  A row is cut into blocks of 32 channels.  b: biased fp32 exponent of the block's largest magnitude, at
 // least 1, or 255 where the block has an infinity or a NaN; a channel is q * 2^(b - 133).
-// q has 7 bits and a sign, the step is a power of two: the value is exact in fp16, bf16 and fp32 alike (the step of an fp16
-// block is below fp16's smallest number only where every product is a multiple of that number), so a kernel that reads a
-// checkpoint sees what it would see in the unpacked tensor.
+// q has 7 bits and a sign, the step is a power of two: the value is exact in fp32, in bf16 and in the tensor's own type (the step of an fp16
+// block is below fp16's smallest number only where every product is a multiple of that number).  Read as fp16, a checkpoint of an fp32
+// or bf16 tensor may have values that fp16 rounds or has no number for.
 constexpr int kQ8Block = 32;
 
 struct Q8Ref {  // a checkpoint: [rows][C] and [rows][ceil(C / 32)]

@@ -29,20 +29,24 @@ __device__ __forceinline__ void load_byte_to_lds(u32x4 rsrc, unsigned voff, unsi
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_ubyte %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
 }
 
-// 16 channels of a checkpoint, of exponent b, as T: exact.
+// 16 channels of a checkpoint, of exponent b, as T: q * 2^(b - 133), rounded where T asks for it.
 template <typename T> __device__ __forceinline__ void widen16(u32x4 q, unsigned b, u32x4 (&out)[2]);
 template <> __device__ __forceinline__ void widen16<_Float16>(u32x4 q, unsigned b, u32x4 (&out)[2]) {
-  // a byte q + 128 as the low bits of a half in [16, 32): 16 + (q + 128) / 64.  Less 18 that is q / 64, times 2^(b - 127): the factor
-  // is a half (subnormal down to 2^-24) for all that a half can be, zero below and infinite above.
-  const _Float16 s = (_Float16)(b == 255u ? __builtin_nanf("") : __builtin_bit_cast(float, b << 23));
-  const f16x2 scale = {s, s}, less = {(_Float16)-18.f, (_Float16)-18.f};
+  // A byte q + 128 as the low bits of a half in [16, 32): 16 + (q + 128) / 64; less 18 that is q / 64.  Times 2^e, e = b - 127, in two
+  // factors of about half of e each, as 2^e may be beyond a half where some products are not (q = 1 of b = 143 is 1024, q = 127 of
+  // b = 102 rounds to 2^-24) and q = 0 has to stay 0.  The first product, with the 18 taken off in the same operation, is exact (multiples
+  // of 2^-19 below 2^12), so only the second one rounds.  Below e = -26 every product is 0, above 22 all but that of q = 0 are infinite.
+  const int e = min(max((int)b - 127, -26), 22), e1 = e >> 1, e2 = e - e1;
+  const auto half2 = [](unsigned bits) { return __builtin_bit_cast(f16x2, bits * 0x10001u); };
+  const f16x2 s1 = half2((unsigned)(e1 + 15) << 10), less = half2(0x8000u | (unsigned)(e1 + 19) << 10 | 0x80u);  // 2^e1, -18 * 2^e1
+  const f16x2 s2 = half2(b == 255u ? 0x7E00u : (unsigned)(e2 + 15) << 10);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const unsigned u = q[w] ^ 0x80808080u;
     const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x4C4C4C4Cu, u, 0x04010400u));
     const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x4C4C4C4Cu, u, 0x04030402u));
-    out[w / 2][w % 2 * 2] = __builtin_bit_cast(unsigned, (lo + less) * scale);
-    out[w / 2][w % 2 * 2 + 1] = __builtin_bit_cast(unsigned, (hi + less) * scale);
+    out[w / 2][w % 2 * 2] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(lo, s1, less) * s2);
+    out[w / 2][w % 2 * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(hi, s1, less) * s2);
   }
 }
 template <int I> __device__ __forceinline__ float byte_value(unsigned w) {  // (one instruction; spelled out it came as two)
