@@ -370,7 +370,10 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
  *   stats            device fp32 [rows][2] receives (m, r) of each row for the backward pass; may be NULL
  *   keep_x, keep_y   receive checkpoints of x and of y (as written) in the same pass: what spconv_q8_pack makes of them;
  *                    each may be NULL, in memory of its own
- * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  mean((x - m)^2) + eps counts as 2^-126 where it is less.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
+ * All arithmetic is fp32, rounded once; a row's values depend on that row alone.  The mean is corrected by the mean of the differences from
+ * it: a row without variance gives x - m = 0 and y = act(bias + residual), whatever its value, and an offset far above a row's spread costs
+ * what fp32 differences cost.  mean((x - m)^2) + eps counts as 2^-126 where it is less; where the sum of squares overflows (differences from
+ * about 2^64 on), r is 0.  C is 1 to 4096, rows * C at most 2^40.  Enqueues on
  * `stream` and allocates nothing.  EINVAL: null pointers, sizes, dtype, relu, eps negative or NaN, one place for
  * two checkpoints. */
 SPCONV_API int spconv_layer_norm_fwd(const void* x, const void* residual_or_null, const float* weight_or_null,

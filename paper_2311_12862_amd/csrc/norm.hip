@@ -3,8 +3,12 @@
 //   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), y = act((x - m) r w + b + res)
 //
 // A group of L lanes holds one row in registers, so every tensor crosses the memory once; statistics are taken in two passes
-// over the registers, in fp32.  Memory bounds it: 300k rows of 256 bf16 with a residual 85 us, 5.4 TB/s; 100k rows of 64 f16 with
-// both checkpoints 10.9 us; 300k of 256 f16 with both 98 (103 where 8-bit rounding took 9 instructions an element), 4.8 TB/s.
+// over the registers, in fp32.  A first mean m0 is off by its sum's roundings, in units of the values' last place, which r would blow up
+// where the offset is far above the spread (60000 throughout, 13 wide: y of 0.78 and not 0).  So d = mean(x - m0) goes
+// with the squares, m = m0 + d, and mean((x - m)^2) = mean((x - m0)^2) - d^2: a row without variance has x - m = 0.  The correction costs
+// 0 to 5 % (170k x 450 f16 73.4 us without, 75.8; 100k x 64 f16 with both checkpoints 9.0, 9.4).
+// Memory bounds it: 300k rows of 256 bf16 with a residual 86 us, 5.4 TB/s; 300k of 256 f16 with both checkpoints 100, 4.7 TB/s (5 more
+// where 8-bit rounding took 9 instructions an element and not 6).
 #include "common.h"
 #include "rows.h"
 
@@ -28,14 +32,21 @@ struct FwdArgs {
 
 // Workgroups a CU is to hold where a lane has one vector.  Scalar registers decide it (masks of lanes, bases of nine tensors): a wave of
 // eight has 80 of them, which the count of resident workgroups leaves out.  For want of 2 to 30 of them launches of eight ran as seven or
-// six, with a second round (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us: fp32 256 wide 81, 102, 110,
+// six, with a second round (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us, before the mean was corrected: fp32 256 wide 81, 102, 110,
 // bounded 58, 73, 83; fp16 450 wide 108, 133, 167, bounded 72, 95, 128; fp32 512 wide 85, 89, 103, bounded 62, 70, 83).
 template <int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E != kBelowVector ? 8 : 0;
+
+// s / c rounded to nearest, inv = 1 / c rounded to nearest (P. Markstein, 1990: one step from the product).  What the correction rests
+// on: c equal differences have their own value as the mean.
+__device__ __forceinline__ float over(float s, float c, float inv) {
+  const float q = s * inv, rest = __builtin_fmaf(-q, c, s);
+  return rest == rest ? __builtin_fmaf(rest, inv, q) : q;  // (squares that overflow stay infinite)
+}
 
 template <typename T, int L, int NV, Ends E>
 __global__ void __launch_bounds__(256, (kFwdHeld<NV, E> ? kFwdHeld<NV, E> : 1)) k_norm_fwd(const FwdArgs p) {
   constexpr int W = Row<T>::W, R = 256 / L;
-  __shared__ float part[2][4];
+  __shared__ float part[3][4];
   const int lane = threadIdx.x % L, rl = threadIdx.x / L;
   const int C = p.C;
   const float inv = 1.f / (float)C;
@@ -73,20 +84,31 @@ __global__ void __launch_bounds__(256, (kFwdHeld<NV, E> ? kFwdHeld<NV, E> : 1)) 
 #pragma unroll
       for (int i = 0; i < W; ++i) sum += x[v][i];
     }
-    const float mean = group_sum<L>(sum, part, 0) * inv;
-    float sq = 0.f;
+    const float first = group_sum<L>(sum, part, 0) * inv;
+    float d = 0.f, sq = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const float m = at[v].live ? mean : 0.f;
+      const float m = at[v].live ? first : 0.f;
 #pragma unroll
       for (int i = 0; i < W; ++i) x[v][i] -= m;
       own_only<E>(at[v], x[v]);
 #pragma unroll
-      for (int i = 0; i < W; ++i) sq += x[v][i] * x[v][i];
+      for (int i = 0; i < W; ++i) {
+        d += x[v][i];
+        sq += x[v][i] * x[v][i];
+      }
     }
+    group_sums<L>(d, sq, part + 1);
+    d = over(d, (float)C, inv);
+    sq = over(sq, (float)C, inv);
+    const float d2 = d * d, var = d2 >= sq ? 0.f : sq - d2;  // (d2 and sq may overflow together; a NaN stays one)
     // (v_rsq is good to one unit of the last place, as its argument is at best; it takes no subnormal numbers)
-    const float rstd = __builtin_amdgcn_rsqf(__builtin_elementwise_maximum(group_sum<L>(sq, part, 1) * inv + p.eps, 0x1p-126f));
-    if (p.stats && row && lane == 0) p.stats[r0 + rl] = make_float2(mean, rstd);
+    const float rstd = __builtin_amdgcn_rsqf(__builtin_elementwise_maximum(var + p.eps, 0x1p-126f));
+    if (p.stats && row && lane == 0) p.stats[r0 + rl] = make_float2(d == d ? first + d : first, rstd);  // (an infinite mean stays one)
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[v][i] -= d;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const bool live = row && at[v].live;

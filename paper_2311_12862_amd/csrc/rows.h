@@ -42,6 +42,26 @@ template <int L> __device__ __forceinline__ float group_sum(float v, float (*par
     return v;
   }
 }
+// Two sums at once, through two slots of their own and one barrier.
+template <int L> __device__ __forceinline__ void group_sums(float& a, float& b, float (*part)[4]) {
+  a = lanes_sum<(L < 64 ? L : 64)>(a);
+  b = lanes_sum<(L < 64 ? L : 64)>(b);
+  if constexpr (L > 64) {
+    if (threadIdx.x % 64 == 0) {
+      part[0][threadIdx.x / 64] = a;
+      part[1][threadIdx.x / 64] = b;
+    }
+    __syncthreads();
+    const int first = threadIdx.x / L * (L / 64);
+    a = part[0][first];
+    b = part[1][first];
+#pragma unroll
+    for (int w = 1; w < L / 64; ++w) {
+      a += part[0][first + w];
+      b += part[1][first + w];
+    }
+  }
+}
 template <int L, int O = 1> __device__ __forceinline__ unsigned group_max(unsigned v) {
   if constexpr (O >= L) return v;
   else return group_max<L, O * 2>(max(v, lane_across<O>(v)));
