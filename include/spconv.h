@@ -356,8 +356,9 @@ SPCONV_API int spconv_relu_bwd_q8(const void* dout, const spconv_q8* kept, void*
 
 /* spconv_wgrad with the layer's input kept as a checkpoint [n_in][C_in]; dtype is that of dout, and the values are read as dtype: the
  * result is that of spconv_wgrad on the tensor that spconv_q8_unpack makes.  16-bit layers on kmaps of K < 5 gather data itself where it is 4-byte aligned
- * (narrow ones on dense maps, whose gradient comes from the map, do not); others unpack it first, into memory that the kmap then keeps (one
- * call before a capture makes it). */
+ * (narrow ones on dense maps, whose gradient comes from the map, do not); others unpack it first, into memory that the kmap then keeps: as
+ * much as the largest such tensor takes, and what captured calls used before a larger one took its place (one call before a capture
+ * makes it). */
 SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_kmap* km, int C_in, int C_out, spconv_dtype dtype,
                                const spconv_config* cfg_or_null, float* dweights, void* stream);
 

@@ -764,15 +764,8 @@ SPCONV_API int spconv_wgrad_q8(const spconv_q8* kept, const void* dout, spconv_k
       return wgrad_run(km, *pl, c.wgrad_pairs, nullptr, kept, dout, C_in, C_out, dtype, dweights, st);
     }
   }
-  const size_t bytes = std::max<size_t>(16, (size_t)km->n_in * C_in * (dtype == SPCONV_F32 ? 4 : 2));
-  if (!km->unpacked || km->unpacked->buf.bytes < bytes) {
-    std::unique_ptr<spconv_kmap::Unpacked> room(new (std::nothrow) spconv_kmap::Unpacked());
-    if (!room) return SPCONV_ENOMEM;
-    SPC_TRY(room->buf.alloc(bytes));
-    room->smaller = std::move(km->unpacked);
-    km->unpacked = std::move(room);
-  }
-  void* x = km->unpacked->buf.p;
+  SPC_TRY(km->unpacked.reserve((size_t)km->n_in * C_in * (dtype == SPCONV_F32 ? 4 : 2), st));
+  void* x = km->unpacked.as<void>();
   if (km->n_in > 0) SPC_TRY(q8_unpack(kept, km->n_in, C_in, dtype, x, st));
   return spconv_wgrad(x, dout, km, C_in, C_out, dtype, cfg, dweights, stream);
 }

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <map>
 #include <memory>
+#include <new>
+#include <utility>
 #include <vector>
 
 #include "spconv.h"
@@ -68,6 +70,38 @@ struct DevBuf {
   }
   int reserve(size_t n) { return (n <= bytes && p) ? SPCONV_OK : alloc(n); }
   template <typename T> T* as() const { return reinterpret_cast<T*>(p); }
+};
+
+// Memory of a kmap that its calls use one after another: as much as the largest of them asked for.  What a captured call has used stays
+// when a larger room takes its place, as the call's graph may replay on it; other memory is given back first.
+class Room {
+ public:
+  int reserve(size_t n, hipStream_t st) {
+    if (n > buf_.bytes || !buf_.p) {
+      if (captured_) {
+        std::unique_ptr<Replayed> r(new (std::nothrow) Replayed());
+        if (!r) return SPCONV_ENOMEM;
+        std::swap(r->buf.p, buf_.p);
+        std::swap(r->buf.bytes, buf_.bytes);
+        r->before = std::move(replayed_);
+        replayed_ = std::move(r);
+        captured_ = false;
+      }
+      SPC_TRY(buf_.alloc(n));
+    }
+    if (!captured_) captured_ = capturing(st);
+    return SPCONV_OK;
+  }
+  template <typename T> T* as() const { return buf_.as<T>(); }
+
+ private:
+  struct Replayed {
+    DevBuf buf;
+    std::unique_ptr<Replayed> before;
+  };
+  DevBuf buf_;
+  bool captured_ = false;
+  std::unique_ptr<Replayed> replayed_;
 };
 
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -161,12 +195,7 @@ struct spconv_kmap {
   // the parts of a split.  Offset k of the whole map is offset k % 25 of plane k / 25.
   std::vector<std::unique_ptr<spconv_kmap>> groups;
   spc::DevBuf scratch;    // split partial sums / wgrad partial tiles
-  // The tensor of a checkpoint that wgrad reads.  Smaller ones that it took the place of stay: a captured graph may replay on them.
-  struct Unpacked {
-    spc::DevBuf buf;
-    std::unique_ptr<Unpacked> smaller;
-  };
-  std::unique_ptr<Unpacked> unpacked;
+  spc::Room unpacked;     // the tensor of a checkpoint that wgrad reads
   // build whose status was not read yet: the pinned block the probe kernel publishes flags and
   // pair count to, with the event that marks the probe's completion
   void* pending_host = nullptr;
