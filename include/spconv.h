@@ -49,7 +49,9 @@
  * caller (the library never frees caller memory); tensors are row-major and
  * contiguous, feature rows 16-byte aligned.  The opaque spconv_kmap owns all
  * of its buffers (hash table, maps, masks, permutations, cached reordered
- * maps, scratch) and releases them in spconv_kmap_destroy.  A kmap caches
+ * maps, scratch) and releases them in spconv_kmap_destroy.  Scratch is as
+ * large as the largest call asked for; what a captured call used stays until
+ * the kmap goes, whatever later calls ask for.  A kmap caches
  * derived data on first use, so concurrent calls on ONE kmap from several
  * host threads or several streams are not supported.
  *

@@ -352,7 +352,7 @@ int run_planes(spconv_op op, const void* src, const void* weights, spconv_kmap* 
     SPC_TRY(plan_get(sub, sub->out_side, c.n_split, plan_flags(c), st, &ls[(size_t)g].plan));
     parts_total += ls[(size_t)g].plan->parts;
   }
-  SPC_TRY(km->scratch.reserve((size_t)parts_total * rows * c_dst * sizeof(float)));
+  SPC_TRY(km->scratch.reserve((size_t)parts_total * rows * c_dst * sizeof(float), st));
   int part0 = 0;
   for (int g = 0; g < n_planes; ++g) {
     spconv_kmap* sub = km->groups[(size_t)g].get();
@@ -450,7 +450,7 @@ int run_igemm_op(spconv_op op, const void* src, const void* weights, spconv_kmap
       SPC_TRY(static_scratch(&ptr));
       a.partial = reinterpret_cast<float*>(ptr);
     } else {
-      SPC_TRY(km->scratch.reserve(need));
+      SPC_TRY(km->scratch.reserve(need, st));
       a.partial = km->scratch.as<float>();
     }
     a.out = nullptr;

@@ -47,7 +47,7 @@ class StreamScope {
   hipStream_t saved_;
 };
 
-// Owning device buffer (grow-only when used as scratch).
+// Owning device buffer.
 struct DevBuf {
   void* p = nullptr;
   size_t bytes = 0;
@@ -68,7 +68,6 @@ struct DevBuf {
     bytes = n;
     return SPCONV_OK;
   }
-  int reserve(size_t n) { return (n <= bytes && p) ? SPCONV_OK : alloc(n); }
   template <typename T> T* as() const { return reinterpret_cast<T*>(p); }
 };
 
@@ -194,7 +193,7 @@ struct spconv_kmap {
   // every kernel runs on a plane as it runs on a 27-offset map; the planes' results are summed like
   // the parts of a split.  Offset k of the whole map is offset k % 25 of plane k / 25.
   std::vector<std::unique_ptr<spconv_kmap>> groups;
-  spc::DevBuf scratch;    // split partial sums / wgrad partial tiles
+  spc::Room scratch;      // split partial sums / wgrad partial tiles
   spc::Room unpacked;     // the tensor of a checkpoint that wgrad reads
   // build whose status was not read yet: the pinned block the probe kernel publishes flags and
   // pair count to, with the event that marks the probe's completion

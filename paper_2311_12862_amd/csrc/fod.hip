@@ -402,7 +402,7 @@ int fod_run(spconv_kmap* km, const ItemPlan& wp, const IgemmArgs& a, int tile_m,
   p.c_red = a.dgrad ? a.C_out : a.C_in;
   p.c_out = a.dgrad ? a.C_in : a.C_out;
   const size_t acc_bytes = (size_t)rows_dst * p.c_out * sizeof(float);
-  SPC_TRY(km->scratch.reserve(acc_bytes));
+  SPC_TRY(km->scratch.reserve(acc_bytes, st));
   {
     const long long n4 = (long long)(acc_bytes / 16);  // channel counts are multiples of 8
     const unsigned blocks = (unsigned)std::min<long long>(ceil_div(n4, 256), 4096);

@@ -711,7 +711,7 @@ int wgrad_map_run(spconv_kmap* km, const void* feats, const void* dout, int C_in
   const int V = km->V, types = (int)ceil_div(V, kMapOffsets), groups = 256 / types;  // one workgroup per CU
   WgradMapParams p{};
   const long long elems = (long long)V * C_in * C_out;
-  SPC_TRY(km->scratch.reserve((size_t)groups * elems * sizeof(float)));
+  SPC_TRY(km->scratch.reserve((size_t)groups * elems * sizeof(float), st));
   p.feats = feats;
   p.dout = dout;
   p.map = km->out_side.map.as<int>();
@@ -765,7 +765,7 @@ int wgrad_run(spconv_kmap* km, const PairList& pl, int64_t piece_pairs, const vo
   } else {
     p.split = split_for(t, ceil_div(C_in, tile) * ceil_div(C_out, tile), V, pl.cap);
   }
-  SPC_TRY(km->scratch.reserve((size_t)p.split.pieces * elems * sizeof(float)));
+  SPC_TRY(km->scratch.reserve((size_t)p.split.pieces * elems * sizeof(float), st));
   p.feats = kept ? kept->data : feats;
   if (kept) {
     p.exps = kept->exps;
