@@ -593,7 +593,7 @@ class Checkpoint:
     """An activation [rows, channels] kept in 8 bits (spconv_q8): data int8 [rows, channels], exps uint8
     [rows, ceil(channels / 32)].  What a backward pass reads an activation for takes a Checkpoint in its place: `wgrad`,
     `layer_norm_bwd` and the gradient through a ReLU, `ew(EW_RELU_BWD, ...)`."""
-    __slots__ = ("rows", "channels", "byref", "_data", "_exps")   # byref: the spconv_q8 of it, for the C calls
+    __slots__ = ("rows", "channels", "byref", "_room", "_tensors")   # byref: the spconv_q8 of it, for the C calls
 
     def __init__(self, data, exps):
         _dev_tensor(data, torch.int8)
@@ -603,7 +603,7 @@ class Checkpoint:
         if data.device != exps.device:
             raise ValueError(f"tensors on {data.device} and {exps.device}")
         self.rows, self.channels = data.shape
-        self._data, self._exps = data, exps
+        self._room, self._tensors = data, (data, exps)
         self.byref = C.byref(Q8(_ptr(data), _ptr(exps)))
 
     @classmethod
@@ -614,41 +614,42 @@ class Checkpoint:
         self = cls.__new__(cls)
         self.rows, self.channels = rows, channels
         at = (rows * channels + 15) // 16 * 16
-        self._data = torch.empty((at + rows * (-(-channels // 32)),), dtype=torch.int8, device=device)
-        self._exps = at
-        if not self._data.is_cuda:
+        self._room = torch.empty((at + rows * (-(-channels // 32)),), dtype=torch.int8, device=device)
+        self._tensors = None
+        if not self._room.is_cuda:
             raise ValueError(f"expected a device, got {device}")
-        base = self._data.data_ptr()
+        base = self._room.data_ptr()
         self.byref = C.byref(Q8(base or None, base + at or None))
         return self
 
     def _views(self):
-        if not isinstance(self._exps, torch.Tensor):
-            room, at = self._data, self._exps
-            self._exps = room[at:].view(torch.uint8).view(self.rows, -1) if self.rows else room.view(torch.uint8).view(0, -(-self.channels // 32))
-            self._data = room[:self.rows * self.channels].view(self.rows, self.channels)
+        """(data, exps); made when they are asked for, and there for other threads once both are."""
+        views = self._tensors
+        if views is None:
+            rows, channels, room = self.rows, self.channels, self._room
+            size = rows * channels
+            exps = room[(size + 15) // 16 * 16:].view(torch.uint8).view(rows, -(-channels // 32))
+            self._tensors = views = room[:size].view(rows, channels), exps
+        return views
 
     @property
     def data(self):
-        self._views()
-        return self._data
+        return self._views()[0]
 
     @property
     def exps(self):
-        self._views()
-        return self._exps
+        return self._views()[1]
 
     @property
     def device(self):
-        return self._data.device
+        return self._room.device
 
     def get_device(self) -> int:
-        return self._data.get_device()
+        return self._room.get_device()
 
     def record_stream(self, stream):
-        self._data.record_stream(stream)
-        if isinstance(self._exps, torch.Tensor):
-            self._exps.record_stream(stream)
+        for t in self._tensors or (self._room,):
+            t.record_stream(stream)
 
 
 def q8_pack(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
@@ -676,7 +677,7 @@ def q8_unpack(kept: Checkpoint, dtype, out=None, stream=None):
         return _elsewhere(dev, stream, q8_unpack, kept, dtype, out)
     rows, channels = kept.rows, kept.channels
     if out is None:
-        out = kept._data.new_empty((rows, channels), dtype=dtype)
+        out = kept._room.new_empty((rows, channels), dtype=dtype)
     else:
         _out_tensor(out, (rows, channels), dtype, kept)
     status = (_LIB or load_library()).spconv_q8_unpack(kept.byref, rows, channels, dt, out.data_ptr() or None,
