@@ -7,8 +7,7 @@ Stream ordering: every call enqueues its work on `stream` (default: torch's
 current stream) and returns without waiting.  A tensor that a call returns or
 fills is therefore ordered on that stream only: read it on the same stream, or
 synchronise that stream first (`tensor.cpu()` runs on torch's current stream).
-Layer norm and the calls on checkpoints take their results' memory and their
-workspaces from torch's pool of the stream that they run on.
+The memory of what a call returns comes from torch's pool of that stream.
 """
 from __future__ import annotations
 
@@ -177,6 +176,56 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _device_now():
+    """Number of the current device (a look-up, as in _current_stream)."""
+    global _device_now
+    torch.cuda.current_device()   # (initialises the device if nothing has yet)
+    _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _device_now()
+
+
+def _stream_here(dev):
+    """_stream(None) where the current device's number is known."""
+    return _raw_stream(dev) if _raw_stream is not None else _stream(None)
+
+
+def _elsewhere(dev, stream, call, *args):
+    """call(*args) with device dev current, and on it `stream` unless that is None.  What the call allocates then comes from the pool
+    of the stream that uses it: a block of another stream's pool may still be read or written by that one's kernels.  The tensors that it
+    returns may be read on the stream that was current before as well, once the caller has ordered the two; torch is told, so that it
+    keeps a block that is given back until that stream is done with it."""
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {dev}")
+    if dev != _device_now():
+        with torch.cuda.device(dev):
+            return _elsewhere(dev, stream, call, *args)
+    handle = None if stream is None else _stream(stream)
+    if handle is None or handle == _stream_here(dev):
+        return call(*args)
+    before = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)):
+        made = call(*args)
+    for t in made if isinstance(made, tuple) else (made,):
+        if t is not None:
+            t.record_stream(before)
+    return made
+
+
+def _made_on(stream, like, shape, dtype):
+    """The tensor that a call on `stream` is to fill (_elsewhere)."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    return _elsewhere(like.get_device(), stream, lambda: like.new_empty(shape, dtype=dtype))
+
+
+def _ints_on(stream, shape):
+    make = lambda: torch.empty(shape, dtype=torch.int32, device=_CUDA)
+    return make() if stream is None else _elsewhere(_device_now(), stream, make)
+
+
 def _cfg(cfg):
     return None if cfg is None else C.byref(cfg)
 
@@ -233,24 +282,24 @@ class KMap:
         return v.value
 
     def out_coords(self, stream=None):
-        dst = torch.empty((self.n_out, 4), dtype=torch.int32, device=_CUDA)
+        dst = _ints_on(stream, (self.n_out, 4))
         _check(load_library().spconv_kmap_out_coords(self.handle, _ptr(dst), _stream(stream)), "spconv_kmap_out_coords")
         return dst
 
     def in_coords(self, stream=None):
-        dst = torch.empty((self.n_in, 4), dtype=torch.int32, device=_CUDA)
+        dst = _ints_on(stream, (self.n_in, 4))
         _check(load_library().spconv_kmap_in_coords(self.handle, _ptr(dst), _stream(stream)), "spconv_kmap_in_coords")
         return dst
 
     def export(self, stream=None):
-        dst = torch.empty((self.n_out, self.V), dtype=torch.int32, device="cuda")
+        dst = _ints_on(stream, (self.n_out, self.V))
         _check(load_library().spconv_kmap_export(self.handle, _ptr(dst), _stream(stream)), "spconv_kmap_export")
         return dst
 
     def export_mask(self, stream=None):
         # bit patterns of uint32; K = 5: four words per row (bit k of the mask is bit k % 32 of word k // 32)
         shape = (self.n_out, 4) if self.K == 5 else (self.n_out,)
-        dst = torch.empty(shape, dtype=torch.int32, device="cuda")
+        dst = _ints_on(stream, shape)
         _check(load_library().spconv_kmap_export_mask(self.handle, _ptr(dst), _stream(stream)), "spconv_kmap_export_mask")
         return dst
 
@@ -262,7 +311,7 @@ class KMap:
 
     def export_perm(self, op, cfg, split, stream=None):
         rows = self.n_out if op == OP_FWD else self.n_in
-        dst = torch.empty((rows,), dtype=torch.int32, device="cuda")
+        dst = _ints_on(stream, (rows,))
         _check(load_library().spconv_kmap_export_perm(self.handle, op, _cfg(cfg), split, _ptr(dst), _stream(stream)),
                "spconv_kmap_export_perm")
         return dst
@@ -337,7 +386,7 @@ def fwd(feats, weights, kmap: KMap, cfg: Config | None = None, out=None, stream=
     if V != kmap.V or c_in != feats.shape[1]:
         raise SpconvError(-5, "weights shape does not fit")
     if out is None:
-        out = feats.new_empty((kmap.n_out, c_out))
+        out = _made_on(stream, feats, (kmap.n_out, c_out), feats.dtype)
     else:
         _out_tensor(out, (kmap.n_out, c_out), feats.dtype, feats)
     status = _LIB.spconv_fwd(_ptr(feats), _ptr(weights), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
@@ -366,7 +415,7 @@ def dgrad(dout, weights, kmap: KMap, cfg: Config | None = None, out=None, stream
     if V != kmap.V or c_out != dout.shape[1]:
         raise SpconvError(-5, "weights shape does not fit")
     if out is None:
-        out = dout.new_empty((kmap.n_in, c_in))
+        out = _made_on(stream, dout, (kmap.n_in, c_in), dout.dtype)
     else:
         _out_tensor(out, (kmap.n_in, c_in), dout.dtype, dout)
     status = _LIB.spconv_dgrad(_ptr(dout), _ptr(weights), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
@@ -386,7 +435,7 @@ def wgrad(feats, dout, kmap: KMap, cfg: Config | None = None, out=None, stream=N
         raise SpconvError(-5, "dout rows do not fit the kmap")
     c_in, c_out = feats.shape[1], dout.shape[1]
     if out is None:
-        out = feats.new_empty((kmap.V, c_in, c_out), dtype=torch.float32)
+        out = _made_on(stream, feats, (kmap.V, c_in, c_out), torch.float32)
     else:
         _out_tensor(out, (kmap.V, c_in, c_out), torch.float32, feats)
     status = _LIB.spconv_wgrad(_ptr(feats), _ptr(dout), kmap.handle, c_in, c_out, dt, _cfg(cfg), _ptr(out),
@@ -471,7 +520,7 @@ def ew(op: int, a, b=None, out=None, stream=None):
         if b.shape != a.shape:
             raise ValueError("shape mismatch")
     if out is None:
-        out = torch.empty_like(a)
+        out = _made_on(stream, a, a.shape, a.dtype)
     status = load_library().spconv_ew(op, _ptr(a), _ptr(b), _ptr(out), a.numel(), _DTYPES[a.dtype], _stream(stream))
     if status:
         _check(status, "spconv_ew")
@@ -513,44 +562,6 @@ def copy_cols(src, src_off: int, dst, dst_off: int, cols: int, stream=None):
 # ---- layer norm and 8-bit checkpoints ------------------------------------------------------------
 # A call of these takes 6 to 14 us on the host (two of each three go to torch's allocations and the launches), more than many of
 # their kernels: checks read a tensor's attributes once, and the device is switched only where it is another one.
-
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
-def _device_now():
-    """Number of the current device (a look-up, as in _current_stream)."""
-    global _device_now
-    torch.cuda.current_device()   # (initialises the device if nothing has yet)
-    _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    return _device_now()
-
-
-def _stream_here(dev):
-    """_stream(None) where the current device's number is known."""
-    return _raw_stream(dev) if _raw_stream is not None else _stream(None)
-
-
-def _elsewhere(dev, stream, call, *args):
-    """call(*args) with device dev current, and on it `stream` unless that is None.  What the call allocates then comes from the pool
-    of the stream that uses it: a block of another stream's pool may still be read or written by that one's kernels.  The tensors that it
-    returns may be read on the stream that was current before as well, once the caller has ordered the two; torch is told, so that it
-    keeps a block that is given back until that stream is done with it."""
-    if getattr(stream, "device_index", dev) != dev:
-        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {dev}")
-    if dev != _device_now():
-        with torch.cuda.device(dev):
-            return _elsewhere(dev, stream, call, *args)
-    handle = None if stream is None else _stream(stream)
-    if handle is None or handle == _stream_here(dev):
-        return call(*args)
-    before = torch.cuda.current_stream(dev)
-    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)):
-        made = call(*args)
-    for t in made if isinstance(made, tuple) else (made,):
-        if t is not None:
-            t.record_stream(before)
-    return made
-
 
 def _row_args(x):
     """Data type's number, shape and device of a tensor [rows, channels]; what is none raises."""

@@ -5,6 +5,9 @@ import torch
 SHAPE = (60_001, 64)
 
 
+NAMES = ["fwd", "bwd", "pack", "unpack", "relu", "wgrad", "convolution", "its input gradient", "its weight gradient", "add", "map"]
+
+
 class _Foreign:
     cuda_stream, device_index = 5, 1
 
@@ -39,6 +42,8 @@ def _calls():
     i = torch.arange(SHAPE[0], device="cuda", dtype=torch.int32)
     km = sp.build_kmap(torch.stack([0 * i, i // 256, i % 256, 0 * i], 1).contiguous(), 3, 1)
 
+    k27 = (torch.randn(27, SHAPE[1], SHAPE[1], device="cuda") / 40).half()
+
     def packed(stream):
         made = sp.q8_pack(x, stream=stream)
         return made.data, made.exps
@@ -50,11 +55,16 @@ def _calls():
         "unpack": lambda s: (sp.q8_unpack(kept, torch.float16, stream=s),),
         "relu": lambda s: (sp.ew(sp.EW_RELU_BWD, dout, kept, stream=s),),
         "wgrad": lambda s: (sp.wgrad(kept, dout, km, stream=s),),
+        "convolution": lambda s: (sp.fwd(x, k27, km, stream=s),),
+        "its input gradient": lambda s: (sp.dgrad(dout, k27, km, stream=s),),
+        "its weight gradient": lambda s: (sp.wgrad(x, dout, km, stream=s),),
+        "add": lambda s: (sp.ew(sp.EW_ADD, x, dout, stream=s),),
+        "map": lambda s: (km.export(stream=s), km.export_mask(stream=s), km.out_coords(stream=s), km.in_coords(stream=s)),
     }
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name", ["fwd", "bwd", "pack", "unpack", "relu", "wgrad"])
+@pytest.mark.parametrize("name", NAMES)
 @pytest.mark.parametrize("named", ["stream", "handle"])
 def test_memory_that_the_current_stream_gave_back(name, named):
     """Blocks of every size that the call takes (its workspace's and its results'), given back while the current stream is still to read
@@ -85,7 +95,7 @@ def test_memory_that_the_current_stream_gave_back(name, named):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name", ["fwd", "bwd", "unpack", "relu"])
+@pytest.mark.parametrize("name", ["fwd", "bwd", "unpack", "relu", "convolution", "add"])
 def test_results_given_back_while_the_current_stream_reads_them(name):
     import paper_2311_12862_amd as sp
     call = _calls()[name]
