@@ -33,7 +33,8 @@ struct FwdArgs {
 // Workgroups a CU is to hold where a lane has one vector.  Scalar registers decide it (masks of lanes, bases of nine tensors): a wave of
 // eight has 80 of them, which the count of resident workgroups leaves out.  For want of 2 to 30 of them launches of eight ran as seven or
 // six, with a second round (77M elements in fp16, 38M in fp32, with no checkpoint, of x, of x and y, us, before the mean was corrected: fp32 256 wide 81, 102, 110,
-// bounded 58, 73, 83; fp16 450 wide 108, 133, 167, bounded 72, 95, 128; fp32 512 wide 85, 89, 103, bounded 62, 70, 83).
+// bounded 58, 73, 83; fp16 450 wide 108, 133, 167, bounded 72, 95, 128; fp32 512 wide 85, 89, 103, bounded 62, 70, 83).  The price: kernels of odd widths keep some 30 scalars in lanes of vector registers, and the 16-bit
+// one of 128 lanes 12 bytes a lane in scratch memory.
 template <int NV, Ends E> constexpr int kFwdHeld = NV == 1 && E != kBelowVector ? 8 : 0;
 
 // s / c rounded to nearest, inv = 1 / c rounded to nearest (P. Markstein, 1990: one step from the product).  What the correction rests

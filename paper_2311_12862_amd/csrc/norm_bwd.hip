@@ -7,7 +7,7 @@
 // 8-bit checkpoints.  dw and db: every lane sums its columns over the rows it visits, the groups of a workgroup meet in LDS, the
 // workgroups' sums in a second kernel, each in a fixed order: the same call gives the same bits.
 // Memory bounds it, and its latency: the next row is loaded ahead of the current one's sums (300k rows of 256 bf16, x and gate from
-// checkpoints, with the residual's gradient: 154 -> 113 us, 5.4 TB/s; 9k rows of 256 f16 8 us, the sums 3).
+// checkpoints, with the residual's gradient: 154 -> 113 us, 5.4 TB/s; 9k rows of 256 f16 8 us, the sums 3 to 5).
 #include "common.h"
 #include "rows.h"
 
@@ -223,6 +223,7 @@ int bwd_groups(bool kept, int64_t blocks) { return kept && blocks >= 16 * kBwdGr
 // One workgroup for so few elements (counted with the idle lanes) that a second launch - 4 us on the host with its workspace, 4 to 5 on the
 // GPU - costs more than the wait for one row after the other, up to 16 turns of 0.5 to 0.9 us; it writes dw and db itself.  A call, us, one
 // workgroup and more: 8k elements 11.2, 15.8; 16k f16 of 256 11.1, 15.8; fp32 of 256 12.0, 15.9; 32k fp32 of 64 20, 16.
+// (Calls without dw and db have no second launch to save, and run on one workgroup all the same: 16k f16 of 32 6.5, one row more 5.5.)
 constexpr int64_t kBwdAlone = 16384;
 bool alone(int64_t rows, int C) {
   int wide = 32;
